@@ -367,6 +367,148 @@ int terra_fragment_pack(const terra_geom* g, int dtype, int32_t ranks, int32_t d
 int terra_fragment_unpack(const terra_geom* g, int dtype, int32_t ranks, int32_t dst_rank,
                           int32_t src_rank, const void* frag_buf, void* src_stripe, void* stream);
 
+/* ---------------------------------------------------------------------------
+ * Operators around the attention, for blocks other than the Swin block above:
+ * the root-mean-square norm, the linear layer and rotary positions.  Matrices
+ * are row-major with a row stride in elements (at least the row length); rows
+ * may have any length and start at any multiple of the element size.  Tensors
+ * of 16-byte rows at 16-byte places are the fast case.  No rows or tokens is a
+ * valid call that does nothing (gradients of parameters are then zero).  A
+ * workspace starts at a multiple of 16 bytes, belongs to one call at a time
+ * (two calls that may overlap, or two captured graphs, need one each), and
+ * none of it needs to start at zero.
+ * ------------------------------------------------------------------------- */
+
+/* 8-bit floats with 4 exponent and 3 mantissa bits, largest 448, no infinity.
+ * Taken by the norm's q and by terra_linear_fwd, nowhere else. */
+#define TERRA_E4M3 3
+
+typedef struct terra_rmsnorm_desc {
+  int64_t rows;
+  int32_t cols;
+  float eps;
+  int64_t x_ld, res_ld, z_ld, y_ld, q_ld;   /* row strides of the tensors in use */
+} terra_rmsnorm_desc;
+
+/* z = x + res, rstd = 1 / sqrt(mean(z^2) + eps), y = gain z rstd, over the
+ * `cols` columns of each row, in float32; every output is rounded once (the
+ * norm is that of z before z is rounded).  x and res (nullable: z = x) of
+ * `dtype` (TERRA_F32, TERRA_BF16, TERRA_F16); gain float32 (nullable: ones).
+ * Outputs, each nullable, one at least: z and y of `dtype`, rstd float32 (for
+ * the backward), and q (TERRA_E4M3) with q_scale (float32, one a row):
+ *   q_scale = max(max |y| / 448, 2^-126),  q = y / q_scale to nearest even,
+ * so that q * q_scale stands for y.  A NaN in a row makes its scale and the
+ * row's y NaN.  z may be x or res, and y may be x, in place with the same
+ * stride (not both the same). */
+int terra_rmsnorm_fwd(const terra_rmsnorm_desc* d, int dtype, const void* x, const void* res, const float* gain,
+                      void* z, void* y, void* q, float* q_scale, float* rstd, void* stream);
+
+/* Device workspace terra_rmsnorm_bwd needs for dgain (0 on invalid input). */
+size_t terra_rmsnorm_bwd_workspace_bytes(int64_t rows, int32_t cols);
+
+/* Backward from dy (gradient of y; stride y_ld) and dz (nullable: what reaches
+ * z by the residual stream; stride res_ld), z and rstd as the forward left
+ * them: with g = dy gain and zh = z rstd,
+ *   dx = rstd (g - zh mean(g zh)) + dz   (`dtype`; of x and of res alike; x_ld)
+ *   dgain = sum over rows of dy zh       (float32, cols; overwritten)
+ * dx or dgain may be NULL; workspace is needed with dgain.  dx may be dy or
+ * dz in place.  The sum over rows has a fixed order (bit-reproducible). */
+int terra_rmsnorm_bwd(const terra_rmsnorm_desc* d, int dtype, const void* dy, const void* z, const float* rstd,
+                      const float* gain, const void* dz, void* dx, float* dgain, void* workspace,
+                      size_t workspace_bytes, void* stream);
+
+enum terra_act { TERRA_ACT_NONE = 0, TERRA_ACT_RELU = 1, TERRA_ACT_GELU = 2, TERRA_ACT_SILU = 3 };
+
+typedef struct terra_linear_desc {
+  int64_t M;                               /* tokens                          */
+  int32_t N, K;                            /* outputs, inputs                 */
+  int64_t x_ld, w_ld, y_ld, res_ld, pre_ld, dx_ld, dw_ld;   /* row strides of the tensors in use */
+  int32_t act;                             /* terra_act                       */
+  int32_t out_dtype;                       /* forward: element type of y, res and pre */
+} terra_linear_desc;
+
+/* Workspaces of the linear layer's calls, for these sizes and any strides and
+ * addresses (0 on invalid input; the forward often needs none). */
+size_t terra_linear_fwd_workspace_bytes(int64_t M, int32_t N, int32_t K, int dtype);
+size_t terra_linear_bwd_workspace_bytes(int64_t M, int32_t N, int32_t K, int dtype);
+
+/* t = x w^T + bias, y = act(t) + res.  x is M x K and w N x K of `dtype`:
+ * TERRA_BF16 or TERRA_F16 (out_dtype the same), or TERRA_E4M3 with x_scale
+ * (float32, M) and w_scale (float32, N), whose products are
+ * x w^T x_scale[m] w_scale[n] (out_dtype TERRA_BF16 or TERRA_F16).  Sums are
+ * float32.  bias float32 (N), res M x N, both nullable; pre (nullable, M x N)
+ * receives t for the backward.  GELU is the exact (erf) form, SiLU
+ * t / (1 + exp(-t)).  y may be res in place with the same stride. */
+int terra_linear_fwd(const terra_linear_desc* d, int dtype, const void* x, const float* x_scale, const void* w,
+                     const float* w_scale, const float* bias, const void* res, void* y, void* pre, void* workspace,
+                     size_t workspace_bytes, void* stream);
+
+/* Backward from dy (M x N, stride y_ld; res's gradient is dy itself), with
+ * dt = dy act'(pre):
+ *   dx = dt w (M x K, `dtype`), dw = dt^T x (N x K, dw_dtype: TERRA_F32 or
+ *   `dtype`), dbias = sum over tokens of dt (float32, N)
+ * each nullable, one at least, overwritten.  `dtype` is TERRA_BF16 or
+ * TERRA_F16.  pre is needed unless act is TERRA_ACT_NONE.  dt enters the two
+ * products rounded to `dtype` (exact for TERRA_ACT_NONE), and dbias in
+ * float32.  Sums over tokens have a fixed order (bit-reproducible). */
+int terra_linear_bwd(const terra_linear_desc* d, int dtype, const void* dy, const void* x, const void* w,
+                     const void* pre, void* dx, void* dw, int dw_dtype, float* dbias, void* workspace,
+                     size_t workspace_bytes, void* stream);
+
+#define TERRA_ROPE_MAX_PAIRS 128
+
+enum terra_rope_layout { TERRA_ROPE_INTERLEAVED = 0, TERRA_ROPE_HALF = 1 };
+enum terra_rope_scaling { TERRA_ROPE_PLAIN = 0, TERRA_ROPE_LINEAR = 1, TERRA_ROPE_NTK = 2, TERRA_ROPE_YARN = 3 };
+
+/* Rotary positions.  The first rot_dim channels of a head turn, the rest are
+ * copied.  They hold `axes` equal parts, part a turned by the token's position
+ * along axis a (two axes: row and column of the grid).  Pair i of a part of
+ * `part` channels: channels (2i, 2i+1) (interleaved) or (i, i + part/2) (half),
+ * with the angle position * f_i, f_i = base^(-2i/part), scaled by `factor` s:
+ *   LINEAR  f_i / s
+ *   NTK     base replaced by base * s^(part / (part - 2))
+ *   YARN    f_i (g + (1 - g) / s), g = clamp((r - beta_slow) / (beta_fast -
+ *           beta_slow), 0, 1), r = orig_len f_i / (2 pi) turns over the
+ *           original length; cosine and sine times 0.1 ln(s) + 1
+ * attn_scale > 0 replaces the factor on cosine and sine. */
+typedef struct terra_rope_desc {
+  int32_t head_dim, rot_dim, axes, layout, scaling;
+  double base, factor, orig_len, beta_fast, beta_slow, attn_scale;
+} terra_rope_desc;
+
+/* What a call needs of it, kept by the caller: pairs of one axis, the factor
+ * on cosine and sine, and f_i / (2 pi) in units of 2^-64. */
+typedef struct terra_rope_plan {
+  terra_rope_desc desc;
+  int32_t pairs;
+  float scale;
+  uint64_t turns[TERRA_ROPE_MAX_PAIRS];
+} terra_rope_plan;
+
+/* Fills `plan` (host only). */
+int terra_plan_rope(const terra_rope_desc* d, terra_rope_plan* plan);
+
+typedef struct terra_rope_tensor {
+  const void* in;                          /* tokens x heads x head_dim       */
+  void* out;
+  int32_t heads;
+  int64_t in_token, in_head, out_token, out_head;   /* strides in elements    */
+} terra_rope_tensor;
+
+/* Turns the heads of q and of k (nullable), e.g. in NHWC or as parts of one
+ * projection's output.  pos: int32 tokens x axes on the device, any value; or
+ * NULL: token t of the grid_h x grid_w grid (t taken modulo its tokens) is at
+ * row t / grid_w, column t % grid_w, on one axis at t.  Element types
+ * TERRA_F32, TERRA_BF16, TERRA_F16, angles to float32's precision at any
+ * position.  `out` may be `in` with the same strides.  At most 256 heads of q
+ * and k together. */
+int terra_rope_fwd(const terra_rope_plan* plan, int dtype, int64_t tokens, const int32_t* pos, int32_t grid_h,
+                   int32_t grid_w, const terra_rope_tensor* q, const terra_rope_tensor* k, void* stream);
+
+/* Its adjoint: gradients of the turned q and k to those of q and k. */
+int terra_rope_bwd(const terra_rope_plan* plan, int dtype, int64_t tokens, const int32_t* pos, int32_t grid_h,
+                   int32_t grid_w, const terra_rope_tensor* dq, const terra_rope_tensor* dk, void* stream);
+
 /* Static string naming a status code. */
 const char* terra_status_string(int status);
 

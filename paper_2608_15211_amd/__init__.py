@@ -19,7 +19,10 @@ Entry points (same names as the C ABI):
     terra_fragment_unpack (ragged window assignment and per-rank route),
     terra_block_fwd_workspace_bytes, terra_block_fwd,
     terra_block_bwd_workspace_bytes, terra_block_bwd (the
-    Swin block around the attention: LayerNorm, projections, MLP)
+    Swin block around the attention: LayerNorm, projections, MLP),
+    terra_rmsnorm_fwd, terra_rmsnorm_bwd, terra_linear_fwd, terra_linear_bwd,
+    terra_plan_rope, terra_rope_fwd, terra_rope_bwd and the workspace queries
+    (operators for blocks of other kinds, in operators.py)
 """
 
 import ctypes
@@ -550,3 +553,18 @@ def terra_block_bwd(dx2, x, params, table, g, saved, out=None, workspace=None):
                                  ctypes.byref(gst), _dev(dtab, "dtable", torch.float32, _sizes(gg)[2]),
                                  _dev(workspace, "workspace"), ctypes.c_size_t(workspace.numel()), _stream()))
     return dx, grads, dtab
+
+
+# ---------------------------------------------------------------- operators around the attention
+OPERATORS = ("TERRA_E4M3", "terra_rmsnorm_fwd", "terra_rmsnorm_bwd_workspace_bytes", "terra_rmsnorm_bwd",
+             "terra_linear_fwd_workspace_bytes", "terra_linear_fwd", "terra_linear_bwd_workspace_bytes", "terra_linear_bwd",
+             "terra_plan_rope", "terra_rope_fwd", "terra_rope_bwd")
+
+
+def __getattr__(name):
+    # operators.py needs torch, which importing the package does not
+    if name in OPERATORS:
+        from . import operators
+        globals().update({n: getattr(operators, n) for n in OPERATORS})
+        return globals()[name]
+    raise AttributeError("module %r has no attribute %r" % (__name__, name))

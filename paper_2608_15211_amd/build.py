@@ -18,7 +18,7 @@ LIB = os.path.join(PKG, "libterra_swin.so")
 # bfloat16, 2 float16), so that they build in parallel.
 SOURCES = [("attn.hip", ["-DTERRA_ATTN_T=1"]), ("attn.hip", ["-DTERRA_ATTN_T=2"]), ("attn.hip", ["-DTERRA_ATTN_T=0"]),
            ("route.hip", []), ("attn_win.hip", []), ("dtab.hip", []), ("plan.hip", []), ("block.hip", []),
-           ("abi.hip", [])]
+           ("norm.hip", []), ("linear.hip", []), ("rope.hip", []), ("abi.hip", [])]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [

@@ -4,6 +4,9 @@
 #include <stdarg.h>
 #include <stdint.h>
 #include <stdio.h>
+#include <string.h>
+
+#include <cmath>
 #include <initializer_list>
 #include <mutex>
 #include <string>
@@ -11,6 +14,7 @@
 #include "terra_common.h"
 #include "terra_plan.h"
 #include "terra_block.h"
+#include "terra_ops.h"
 #include "../../include/terra_swin.h"
 
 namespace terra {
@@ -595,6 +599,294 @@ int terra_winattn_bwd_nhwc_noalloc(const terra_geom* g, int dtype, const void* q
   if ((s = scratch_address(&ws))) return s;
   return attn_bwd_common(g, dtype, true, q, k, v, o, o_lo, dout, lse, bias_table, dq, dk, dv,
                          dbias_table, ws, (size_t)TERRA_SCRATCH_BYTES, stream);
+}
+
+// ---- root-mean-square norm ------------------------------------------------
+
+static int check_rms(const terra_rmsnorm_desc* d, int dtype) {
+  if (!d) return fail(TERRA_ERR_INVALID, "descriptor pointer is NULL");
+  int s = check_dtype(dtype);
+  if (s) return s;
+  if (d->rows < 0 || d->cols < 1) return fail(TERRA_ERR_INVALID, "rows must be >= 0 and cols >= 1");
+  if (!(d->eps >= 0.0f && d->eps < INFINITY)) return fail(TERRA_ERR_INVALID, "eps must be finite and >= 0");
+  if (d->cols > (1 << 28)) return fail(TERRA_ERR_UNSUPPORTED, "cols must be at most 2^28");
+  return ok();
+}
+
+// A matrix argument of a call: its name, address (NULL: absent), row stride,
+// row length and element size.
+struct MatArg {
+  const char* name;
+  const void* p;
+  int64_t ld, cols;
+  int esize;
+};
+static int check_mats(std::initializer_list<MatArg> mats) {
+  for (const MatArg& m : mats) {
+    if (!m.p) continue;
+    if (m.ld < m.cols)
+      return fail(TERRA_ERR_INVALID, "row stride %lld of %s is below its row length %lld", (long long)m.ld, m.name,
+                  (long long)m.cols);
+    if (m.ld >= ((int64_t)1 << 40)) return fail(TERRA_ERR_UNSUPPORTED, "row stride of %s is 2^40 or more", m.name);
+    if ((uintptr_t)m.p % m.esize)
+      return fail(TERRA_ERR_INVALID, "%s does not start at a multiple of its element size", m.name);
+  }
+  return ok();
+}
+
+int terra_rmsnorm_fwd(const terra_rmsnorm_desc* d, int dtype, const void* x, const void* res, const float* gain,
+                      void* z, void* y, void* q, float* q_scale, float* rstd, void* stream) {
+  int s = check_rms(d, dtype);
+  if (s) return s;
+  if (d->rows == 0) return ok();
+  if (!x) return fail(TERRA_ERR_INVALID, "x is NULL");
+  if (!q != !q_scale) return fail(TERRA_ERR_INVALID, "q and q_scale come together");
+  if (!z && !y && !q && !rstd) return fail(TERRA_ERR_INVALID, "no output asked for");
+  const int es = dtype == TERRA_F32 ? 4 : 2;
+  if ((s = check_mats({{"x", x, d->x_ld, d->cols, es}, {"res", res, d->res_ld, d->cols, es},
+                       {"z", z, d->z_ld, d->cols, es}, {"y", y, d->y_ld, d->cols, es}, {"q", q, d->q_ld, d->cols, 1},
+                       {"gain", gain, d->cols, d->cols, 4}, {"q_scale", q_scale, 1, 1, 4}, {"rstd", rstd, 1, 1, 4}})))
+    return s;
+  terra::RmsFwd a = {x, res, gain, z, y, (uint8_t*)q, q_scale, rstd, d->rows, d->x_ld, d->res_ld, d->z_ld, d->y_ld,
+                     d->q_ld, d->cols, d->eps};
+  return hip_status(terra::launch_rms_fwd(dtype, a, (hipStream_t)stream), "terra_rmsnorm_fwd launch");
+}
+
+size_t terra_rmsnorm_bwd_workspace_bytes(int64_t rows, int32_t cols) {
+  if (rows < 0 || cols < 1) return 0;
+  return (size_t)terra::rms_bwd_blocks(rows, cols) * cols * sizeof(float);
+}
+
+int terra_rmsnorm_bwd(const terra_rmsnorm_desc* d, int dtype, const void* dy, const void* z, const float* rstd,
+                      const float* gain, const void* dz, void* dx, float* dgain, void* workspace,
+                      size_t workspace_bytes, void* stream) {
+  int s = check_rms(d, dtype);
+  if (s) return s;
+  if (!dx && !dgain) return fail(TERRA_ERR_INVALID, "no output asked for");
+  const int es = dtype == TERRA_F32 ? 4 : 2;
+  if (d->rows > 0) {
+    if (!dy || !z || !rstd) return fail(TERRA_ERR_INVALID, "dy, z or rstd is NULL");
+    if ((s = check_mats({{"dy", dy, d->y_ld, d->cols, es}, {"z", z, d->z_ld, d->cols, es},
+                         {"dz", dz, d->res_ld, d->cols, es}, {"dx", dx, d->x_ld, d->cols, es},
+                         {"gain", gain, d->cols, d->cols, 4}, {"rstd", rstd, 1, 1, 4}})))
+      return s;
+  }
+  if ((s = check_mats({{"dgain", dgain, d->cols, d->cols, 4}}))) return s;
+  if (dgain && d->rows > 0) {
+    const size_t need = terra_rmsnorm_bwd_workspace_bytes(d->rows, d->cols);
+    if (!workspace || workspace_bytes < need)
+      return fail(TERRA_ERR_WORKSPACE, "workspace of %zu bytes needed, %zu given", need, workspace ? workspace_bytes : 0);
+    if ((uintptr_t)workspace % 16) return fail(TERRA_ERR_INVALID, "workspace must be 16-byte aligned");
+  }
+  terra::RmsBwd a = {dy, z, dz, rstd, gain, dx, dgain ? (float*)workspace : nullptr, d->rows, d->y_ld, d->z_ld,
+                     d->res_ld, d->x_ld, d->cols};
+  return hip_status(terra::launch_rms_bwd(dtype, a, dgain, (hipStream_t)stream), "terra_rmsnorm_bwd launch");
+}
+
+// ---- linear layer ---------------------------------------------------------
+
+static int check_linear_size(int64_t M, int32_t N, int32_t K) {
+  if (M < 0 || N < 1 || K < 1) return fail(TERRA_ERR_INVALID, "M must be >= 0, N and K >= 1");
+  if (M >= ((int64_t)1 << 31) - 256 || N > (1 << 28) || K > (1 << 28))
+    return fail(TERRA_ERR_UNSUPPORTED, "M must be below 2^31 - 256, N and K at most 2^28");
+  // workgroups of 512 threads, of which a launch takes fewer than 2^32
+  auto tiles = [](int64_t a, int64_t b) { return ((a + 127) / 128) * ((b + 127) / 128); };
+  if (tiles(M, N) >= (1 << 22) || tiles(M, K) >= (1 << 22) || tiles(N, K) >= (1 << 22))
+    return fail(TERRA_ERR_UNSUPPORTED, "a product of 2^22 or more 128 x 128 tiles is not supported");
+  return ok();
+}
+
+static int check_linear(const terra_linear_desc* d) {
+  if (!d) return fail(TERRA_ERR_INVALID, "descriptor pointer is NULL");
+  int s = check_linear_size(d->M, d->N, d->K);
+  if (s) return s;
+  if (d->act < TERRA_ACT_NONE || d->act > TERRA_ACT_SILU)
+    return fail(TERRA_ERR_INVALID, "act %d is not one of TERRA_ACT_NONE, _RELU, _GELU, _SILU", d->act);
+  return ok();
+}
+
+static int check_linear_ws(size_t need, const void* workspace, size_t bytes) {
+  if (need == 0) return ok();
+  if (!workspace || bytes < need)
+    return fail(TERRA_ERR_WORKSPACE, "workspace of %zu bytes needed, %zu given", need, workspace ? bytes : 0);
+  if ((uintptr_t)workspace % 16) return fail(TERRA_ERR_INVALID, "workspace must be 16-byte aligned");
+  return ok();
+}
+
+size_t terra_linear_fwd_workspace_bytes(int64_t M, int32_t N, int32_t K, int dtype) {
+  if (check_linear_size(M, N, K) || (dtype != TERRA_BF16 && dtype != TERRA_F16 && dtype != TERRA_E4M3)) return 0;
+  return terra::lin_fwd_workspace(M, N, K, dtype);
+}
+
+int terra_linear_fwd(const terra_linear_desc* d, int dtype, const void* x, const float* x_scale, const void* w,
+                     const float* w_scale, const float* bias, const void* res, void* y, void* pre, void* workspace,
+                     size_t workspace_bytes, void* stream) {
+  int s = check_linear(d);
+  if (s) return s;
+  if (dtype != TERRA_BF16 && dtype != TERRA_F16 && dtype != TERRA_E4M3)
+    return dtype == TERRA_F32 ? fail(TERRA_ERR_UNSUPPORTED, "the linear layer takes TERRA_BF16, TERRA_F16 or TERRA_E4M3")
+                              : fail(TERRA_ERR_INVALID, "dtype %d is not an element type", dtype);
+  const bool q = dtype == TERRA_E4M3;
+  if (q ? (d->out_dtype != TERRA_BF16 && d->out_dtype != TERRA_F16) : d->out_dtype != dtype)
+    return fail(TERRA_ERR_INVALID, "out_dtype %d: TERRA_E4M3 operands give TERRA_BF16 or TERRA_F16, others their own type",
+                d->out_dtype);
+  if (d->M == 0) return ok();
+  if (!x || !w || !y) return fail(TERRA_ERR_INVALID, "x, w or y is NULL");
+  if (q ? (!x_scale || !w_scale) : (x_scale || w_scale))
+    return fail(TERRA_ERR_INVALID, "x_scale and w_scale come with TERRA_E4M3 operands, and only with them");
+  const int es = q ? 1 : 2;
+  if ((s = check_mats({{"x", x, d->x_ld, d->K, es}, {"w", w, d->w_ld, d->K, es}, {"y", y, d->y_ld, d->N, 2},
+                       {"res", res, d->res_ld, d->N, 2}, {"pre", pre, d->pre_ld, d->N, 2},
+                       {"bias", bias, d->N, d->N, 4}, {"x_scale", x_scale, 1, 1, 4}, {"w_scale", w_scale, 1, 1, 4}})))
+    return s;
+  if ((s = check_linear_ws(terra::lin_fwd_workspace(d->M, d->N, d->K, dtype), workspace, workspace_bytes))) return s;
+  terra::LinFwd a = {x, w, x_scale, w_scale, bias, res, y, pre, d->M, d->x_ld, d->w_ld, d->y_ld, d->res_ld, d->pre_ld,
+                     d->N, d->K, d->act};
+  return hip_status(terra::launch_lin_fwd(dtype, d->out_dtype, a, workspace, (hipStream_t)stream),
+                    "terra_linear_fwd launch");
+}
+
+size_t terra_linear_bwd_workspace_bytes(int64_t M, int32_t N, int32_t K, int dtype) {
+  if (check_linear_size(M, N, K) || (dtype != TERRA_BF16 && dtype != TERRA_F16)) return 0;
+  return terra::lin_bwd_workspace(M, N, K);
+}
+
+int terra_linear_bwd(const terra_linear_desc* d, int dtype, const void* dy, const void* x, const void* w,
+                     const void* pre, void* dx, void* dw, int dw_dtype, float* dbias, void* workspace,
+                     size_t workspace_bytes, void* stream) {
+  int s = check_linear(d);
+  if (s) return s;
+  if (dtype != TERRA_BF16 && dtype != TERRA_F16)
+    return dtype == TERRA_F32 || dtype == TERRA_E4M3
+               ? fail(TERRA_ERR_UNSUPPORTED, "the linear layer's backward takes TERRA_BF16 or TERRA_F16")
+               : fail(TERRA_ERR_INVALID, "dtype %d is not an element type", dtype);
+  if (!dx && !dw && !dbias) return fail(TERRA_ERR_INVALID, "no output asked for");
+  if (dw && dw_dtype != TERRA_F32 && dw_dtype != dtype)
+    return fail(TERRA_ERR_INVALID, "dw_dtype %d is neither TERRA_F32 nor the element type", dw_dtype);
+  if (d->M > 0) {
+    if (!dy || (dw && !x) || (dx && !w)) return fail(TERRA_ERR_INVALID, "dy, x or w is NULL");
+    if (d->act != TERRA_ACT_NONE && !pre) return fail(TERRA_ERR_INVALID, "pre is NULL, and act is not TERRA_ACT_NONE");
+    if ((s = check_mats({{"dy", dy, d->y_ld, d->N, 2}, {"x", dw ? x : nullptr, d->x_ld, d->K, 2},
+                         {"w", dx ? w : nullptr, d->w_ld, d->K, 2},
+                         {"pre", d->act != TERRA_ACT_NONE ? pre : nullptr, d->pre_ld, d->N, 2},
+                         {"dx", dx, d->dx_ld, d->K, 2}})))
+      return s;
+  }
+  if ((s = check_mats({{"dw", dw, d->dw_ld, d->K, dw_dtype == TERRA_F32 ? 4 : 2}, {"dbias", dbias, d->N, d->N, 4}})))
+    return s;
+  if ((s = check_linear_ws(terra::lin_bwd_workspace(d->M, d->N, d->K), workspace, workspace_bytes))) return s;
+  terra::LinBwd a = {dy, x, w, pre, dx, dw, dbias, d->M, d->y_ld, d->x_ld, d->w_ld, d->pre_ld, d->dx_ld, d->dw_ld,
+                     d->N, d->K, d->act, dw_dtype == TERRA_F32};
+  return hip_status(terra::launch_lin_bwd(dtype, a, workspace, (hipStream_t)stream), "terra_linear_bwd launch");
+}
+
+// ---- rotary positions -----------------------------------------------------
+
+static int check_rope_desc(const terra_rope_desc* d) {
+  if (!d) return fail(TERRA_ERR_INVALID, "descriptor pointer is NULL");
+  if (d->axes != 1 && d->axes != 2) return fail(TERRA_ERR_INVALID, "axes %d is not 1 or 2", d->axes);
+  if (d->head_dim < 2 || d->rot_dim < 2 || d->rot_dim > d->head_dim || d->rot_dim % (2 * d->axes))
+    return fail(TERRA_ERR_INVALID, "rot_dim %d must be a multiple of 2 * axes and at most head_dim %d", d->rot_dim,
+                d->head_dim);
+  if (d->head_dim > 2 * TERRA_ROPE_MAX_PAIRS)
+    return fail(TERRA_ERR_UNSUPPORTED, "head_dim %d is above %d", d->head_dim, 2 * TERRA_ROPE_MAX_PAIRS);
+  if (d->layout != TERRA_ROPE_INTERLEAVED && d->layout != TERRA_ROPE_HALF)
+    return fail(TERRA_ERR_INVALID, "layout %d is not TERRA_ROPE_INTERLEAVED or TERRA_ROPE_HALF", d->layout);
+  if (d->scaling < TERRA_ROPE_PLAIN || d->scaling > TERRA_ROPE_YARN)
+    return fail(TERRA_ERR_INVALID, "scaling %d is not one of TERRA_ROPE_PLAIN, _LINEAR, _NTK, _YARN", d->scaling);
+  if (!(d->base >= 1.0 && d->base <= 1e30)) return fail(TERRA_ERR_INVALID, "base must be between 1 and 1e30");
+  if (d->scaling != TERRA_ROPE_PLAIN && !(d->factor >= 1.0 && d->factor <= 1e9))
+    return fail(TERRA_ERR_INVALID, "factor must be between 1 and 1e9");
+  if (d->scaling == TERRA_ROPE_NTK && d->rot_dim == 2 * d->axes)
+    return fail(TERRA_ERR_INVALID, "TERRA_ROPE_NTK needs two pairs an axis or more");
+  if (d->scaling == TERRA_ROPE_YARN &&
+      !(d->orig_len >= 1.0 && d->orig_len <= 1e18 && d->beta_slow >= 0.0 && d->beta_fast > d->beta_slow && d->beta_fast <= 1e9))
+    return fail(TERRA_ERR_INVALID, "TERRA_ROPE_YARN needs orig_len >= 1 and 0 <= beta_slow < beta_fast");
+  if (!(d->attn_scale >= 0.0 && d->attn_scale <= 1e6))
+    return fail(TERRA_ERR_INVALID, "attn_scale must be between 0 (the scaling's own) and 1e6");
+  return ok();
+}
+
+int terra_plan_rope(const terra_rope_desc* d, terra_rope_plan* plan) {
+  int s = check_rope_desc(d);
+  if (s) return s;
+  if (!plan) return fail(TERRA_ERR_INVALID, "plan pointer is NULL");
+  memset(plan, 0, sizeof(*plan));
+  plan->desc = *d;
+  const int part = d->rot_dim / d->axes;
+  plan->pairs = part / 2;
+  plan->scale = d->attn_scale > 0.0 ? (float)d->attn_scale
+                : d->scaling == TERRA_ROPE_YARN ? (float)(0.1 * log(d->factor) + 1.0) : 1.0f;
+  terra::rope_turns(d->base, d->scaling, d->factor, d->orig_len, d->beta_fast, d->beta_slow, part, plan->turns);
+  return ok();
+}
+
+static int rope_common(const terra_rope_plan* p, int dtype, int64_t tokens, const int32_t* pos, int32_t grid_h,
+                       int32_t grid_w, const terra_rope_tensor* q, const terra_rope_tensor* k, float sign,
+                       void* stream) {
+  if (!p) return fail(TERRA_ERR_INVALID, "plan pointer is NULL");
+  int s = check_rope_desc(&p->desc);
+  if (s) return s;
+  const terra_rope_desc& d = p->desc;
+  if (p->pairs != d.rot_dim / d.axes / 2) return fail(TERRA_ERR_INVALID, "the plan was not made by terra_plan_rope");
+  if ((s = check_dtype(dtype))) return s;
+  if (tokens < 0) return fail(TERRA_ERR_INVALID, "tokens must be >= 0");
+  if (!q) return fail(TERRA_ERR_INVALID, "q is NULL");
+  if (pos) {
+    if ((uintptr_t)pos % 4) return fail(TERRA_ERR_INVALID, "pos does not start at a multiple of its element size");
+  } else {
+    if (grid_h < 1 || grid_w < 1 || (int64_t)grid_h * grid_w >= ((int64_t)1 << 31))
+      return fail(TERRA_ERR_INVALID, "without pos, grid_h and grid_w must be >= 1 and their product below 2^31");
+  }
+  if (tokens >= ((int64_t)1 << 31)) return fail(TERRA_ERR_UNSUPPORTED, "tokens must be below 2^31");
+  terra::RopeArgs a = {};
+  const int es = dtype == TERRA_F32 ? 4 : 2;
+  const terra_rope_tensor* t[2] = {q, k};
+  int heads = 0;
+  for (int i = 0; i < 2; ++i) {
+    if (!t[i]) continue;
+    const char* name = i == 0 ? "q" : "k";
+    if (t[i]->heads < 1) return fail(TERRA_ERR_INVALID, "%s has %d heads", name, t[i]->heads);
+    if (tokens > 0 && (!t[i]->in || !t[i]->out)) return fail(TERRA_ERR_INVALID, "%s: input or output is NULL", name);
+    if (((uintptr_t)t[i]->in | (uintptr_t)t[i]->out) % es)
+      return fail(TERRA_ERR_INVALID, "%s does not start at a multiple of its element size", name);
+    const int64_t in_h = t[i]->in_head, in_t = t[i]->in_token, out_h = t[i]->out_head, out_t = t[i]->out_token;
+    for (int64_t st : {in_h, in_t, out_h, out_t})
+      if (st < 0 || st >= ((int64_t)1 << 31)) return fail(TERRA_ERR_INVALID, "%s: strides must be >= 0 and below 2^31", name);
+    // heads within a token, or tokens within a head
+    const int64_t span_h = (int64_t)(t[i]->heads - 1) * out_h + d.head_dim, span_t = (tokens - 1) * out_t + d.head_dim;
+    if (!((out_h >= d.head_dim || t[i]->heads == 1) && (out_t >= span_h || tokens <= 1)) &&
+        !((out_t >= d.head_dim || tokens <= 1) && (out_h >= span_t || t[i]->heads == 1)))
+      return fail(TERRA_ERR_INVALID, "%s: the output's strides let its heads overlap", name);
+    if (t[i]->in == t[i]->out && (in_h != out_h || in_t != out_t))
+      return fail(TERRA_ERR_INVALID, "%s: in place, input and output must have the same strides", name);
+    a.side[i] = {t[i]->in, t[i]->out, t[i]->heads, in_t, in_h, out_t, out_h};
+    heads += t[i]->heads;
+  }
+  if (heads > 256) return fail(TERRA_ERR_UNSUPPORTED, "more than 256 heads of q and k together");
+  a.tokens = tokens;
+  a.pos = pos;
+  a.axes = d.axes;
+  a.half = p->pairs;
+  a.pairs = d.rot_dim / 2;
+  a.hd = d.head_dim;
+  a.grid_w = (uint32_t)grid_w;
+  a.grid_hw = (uint32_t)grid_h * (uint32_t)grid_w;
+  a.scale = p->scale;
+  a.sin_scale = sign * p->scale;
+  memcpy(a.turns, p->turns, sizeof(a.turns));
+  return hip_status(terra::launch_rope(dtype, a, d.layout == TERRA_ROPE_HALF, (hipStream_t)stream),
+                    sign > 0 ? "terra_rope_fwd launch" : "terra_rope_bwd launch");
+}
+
+int terra_rope_fwd(const terra_rope_plan* plan, int dtype, int64_t tokens, const int32_t* pos, int32_t grid_h,
+                   int32_t grid_w, const terra_rope_tensor* q, const terra_rope_tensor* k, void* stream) {
+  return rope_common(plan, dtype, tokens, pos, grid_h, grid_w, q, k, 1.0f, stream);
+}
+
+int terra_rope_bwd(const terra_rope_plan* plan, int dtype, int64_t tokens, const int32_t* pos, int32_t grid_h,
+                   int32_t grid_w, const terra_rope_tensor* dq, const terra_rope_tensor* dk, void* stream) {
+  return rope_common(plan, dtype, tokens, pos, grid_h, grid_w, dq, dk, -1.0f, stream);
 }
 
 const char* terra_status_string(int status) {

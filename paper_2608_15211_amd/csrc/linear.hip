@@ -1,0 +1,927 @@
+// linear.hip - the linear layer y = act(x W^T + bias) + res and its backward,
+// on the matrix cores: 16-bit operands, or (forward) e4m3 ones with one scale
+// for each row of x and of W.
+//
+// Forms of a product, chosen by size and alignment (launch_lin_fwd):
+// * few tokens (skinny_kernel): W is read once, straight into registers;
+// * 256 x 256 tiles of eight waves, 128 x 128 tiles of four, the latter also
+//   in contraction slices: operands come by direct-to-LDS loads;
+// * 128 x 128 tiles whose operands pass through registers, for rows that do
+//   not start at multiples of 16 bytes or do not hold whole 16-byte chunks.
+// Sums are float32; every output is rounded once.  The matrix cores add 8-bit
+// products eight at a time, aligned to the largest of the eight and cut 13 bits
+// below its leading bit, before these reach the float32 sum: at K = 64 an
+// error of up to 1.8e-5 of the sum of magnitudes, a hundredth of bfloat16's step.
+#include <algorithm>
+#include <type_traits>
+
+#include "terra_gemm.h"
+#include "terra_ops.h"
+#include "terra_vec.h"
+
+namespace terra {
+
+namespace {
+
+struct e4m3 {};
+typedef int i32x8 __attribute__((ext_vector_type(8)));
+
+// Bytes of an element, and its matrix instructions on operands of 32 bytes a
+// lane (two 16-byte pieces of a row; which contraction indices a lane holds
+// does not matter as long as A and B agree).
+template <typename T> struct Elem { static constexpr int kBytes = 2; };
+template <> struct Elem<e4m3> { static constexpr int kBytes = 1; };
+
+constexpr int kUnitScale = 0x7f7f7f7f;     // e8m0 block scales of 1
+
+__device__ inline i32x8 join(const bf16x8& lo, const bf16x8& hi) {
+  const i32x4 a = __builtin_bit_cast(i32x4, lo), b = __builtin_bit_cast(i32x4, hi);
+  return i32x8{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
+}
+
+// One half of a stage (32 contraction indices, of 8-bit elements 64): a
+// wave's MI x 2 blocks of 32 x 32.
+template <typename T, int MI>
+__device__ __forceinline__ void stage_products(f32x16 (&acc)[MI][2], const bf16x8 (&ao)[2][MI],
+                                               const bf16x8 (&bo)[2][2]) {
+  if constexpr (std::is_same<T, e4m3>::value) {
+#pragma unroll
+    for (int i = 0; i < MI; ++i)
+#pragma unroll
+      for (int j = 0; j < 2; ++j)
+        acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(join(ao[0][i], ao[1][i]), join(bo[0][j], bo[1][j]),
+                                                                    acc[i][j], 0, 0, 0, kUnitScale, 0, kUnitScale);
+  } else {
+#pragma unroll
+    for (int c = 0; c < 2; ++c)
+#pragma unroll
+      for (int i = 0; i < MI; ++i)
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+          mma16(acc[i][j], __builtin_bit_cast(typename Operand<T>::type, ao[c][i]),
+                __builtin_bit_cast(typename Operand<T>::type, bo[c][j]));
+  }
+}
+
+// The products of a workgroup tile's `nk` stages into acc.  issue_a(s, st)
+// starts the loads of stage s of A into buffer st of its ring, issue_b those
+// of B; every thread calls both.  Eight waves: the two waves of a SIMD take
+// turns at LDS and the matrix cores; four waves: three stages in flight.
+// (The Swin block's kernel holds the same two schedules and what they were
+// measured against.)
+template <typename T, bool KROW, int NW, class IssueA, class IssueB>
+__device__ __forceinline__ void gemm_stages(bf16* lds, int nk, f32x16 (&acc)[NW == 8 ? 4 : 2][2],
+                                            const IssueA& issue_a, const IssueB& issue_b) {
+  constexpr int NT = NW * 64, BM = NW == 8 ? kBM : kBS, BN = BM, BK = kBK, MI = BM / 64;
+  const int lane = threadIdx.x & 63;
+  const int wave = threadIdx.x >> 6;
+  const int wm = (wave / (NW / 2)) * 32 * MI, wn = (wave % (NW / 2)) * 64;
+  typedef Tile<BM, KROW, BK, NT> TA;
+  typedef Tile<BN, KROW, BK, NT> TB;
+  // LDS rings: kRA stages of A, then two (four waves: four) of B
+  constexpr int kRA = NW == 8 ? 3 : 4;
+  auto a_tile = [&](int st) { return lds + st * TA::kElems; };
+  auto b_tile = [&](int st) { return lds + kRA * TA::kElems + st * TB::kElems; };
+  bf16x8 ao[2][MI], bo[2][2];
+  // operands of the 32 contraction indices from 32 * hf of a stage
+  auto read_ops = [&](const bf16* ta, const bf16* tb, int hf) {
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+      const int k0 = 32 * hf + 16 * c;
+#pragma unroll
+      for (int j = 0; j < 2; ++j)
+        bo[c][j] = KROW ? row_operand<BN, BK>(tb, k0, wn + 32 * j, lane) : tr_operand<BN, BK>(tb, k0, wn + 32 * j, lane);
+#pragma unroll
+      for (int i = 0; i < MI; ++i)
+        ao[c][i] =
+            KROW ? row_operand<BM, BK>(ta, k0, wm + 32 * i, lane) : tr_operand<BM, BK>(ta, k0, wm + 32 * i, lane);
+    }
+  };
+  auto mfmas = [&]() { stage_products<T>(acc, ao, bo); };
+  if constexpr (NW == 8) {
+    // Turn 4 kt + 2 hf: the first half of the workgroup reads half hf of
+    // stage kt, the second half multiplies what it read in its last turn;
+    // in the next turn they swap.  A stage's buffer is free after turn
+    // 4 kt + 3, so the loads of B's stage kt + 1 (two buffers) go out while
+    // half 0 of stage kt is read, those of A's stage kt + 2 (three) while
+    // half 1 is.
+    const bool second = __builtin_amdgcn_readfirstlane(wave) >= NW / 2;
+    if (nk > 0) {
+      issue_a(0, 0);
+      issue_b(0, 0);
+    }
+    if (nk > 1) {
+      issue_a(1, 1);
+      wait_vm<TA::kPer>();
+    } else {
+      wait_vm<0>();
+    }
+    lds_barrier();
+    if (second) lds_barrier();
+    int sa3 = 0;               // kt % 3
+    for (int kt = 0; kt < nk; ++kt) {
+      const bf16* ta = a_tile(sa3);
+      const bf16* tb = b_tile(kt & 1);
+#pragma unroll
+      for (int hf = 0; hf < 2; ++hf) {
+        read_ops(ta, tb, hf);
+        if (hf == 0) {
+          if (kt + 1 < nk) issue_b(kt + 1, (kt + 1) & 1);
+        } else {
+          if (kt + 2 < nk) issue_a(kt + 2, sa3 == 0 ? 2 : sa3 - 1);
+        }
+        auto wait_next = [&]() {     // stage kt + 1 is in LDS (A of stage kt + 2 may be in flight)
+          if (hf == 1) {
+            if (kt + 2 < nk) wait_vm<TA::kPer>();
+            else wait_vm<0>();
+          }
+        };
+        if (second) wait_next();
+        __builtin_amdgcn_sched_barrier(0);
+        lds_barrier();
+        __builtin_amdgcn_sched_barrier(0);
+        __builtin_amdgcn_s_setprio(1);
+        mfmas();
+        __builtin_amdgcn_s_setprio(0);
+        __builtin_amdgcn_sched_barrier(0);
+        if (!second) wait_next();
+        lds_barrier();
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      sa3 = sa3 == 2 ? 0 : sa3 + 1;
+    }
+    if (!second) lds_barrier();
+  } else {
+    constexpr int kLoads = TA::kPer + TB::kPer;
+    for (int s = 0; s < 3; ++s)
+      if (s < nk) { issue_a(s, s); issue_b(s, s); }
+    for (int kt = 0; kt < nk; ++kt) {
+      const int left = nk - 1 - kt;      // stages after this one
+      if (left >= 2) wait_vm<2 * kLoads>();
+      else if (left == 1) wait_vm<kLoads>();
+      else wait_vm<0>();
+      lds_barrier();     // stage kt is in LDS, and every wave is done with the one before
+      if (left >= 3) {
+        issue_a(kt + 3, (kt + 3) & 3);
+        issue_b(kt + 3, (kt + 3) & 3);
+      }
+#pragma unroll
+      for (int hf = 0; hf < 2; ++hf) {
+        read_ops(a_tile(kt & 3), b_tile(kt & 3), hf);
+        mfmas();
+      }
+    }
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Operands of any alignment and length: 16-byte chunks pass through registers
+// (slot q of a tile: thread q % 256), the chunks of stage k + 1 loaded while
+// stage k is multiplied; two buffers, one barrier a stage.
+// ---------------------------------------------------------------------------
+template <bool KROW, int ES>
+struct RegStager {
+  typedef Tile<kBS, KROW, kBK, 256> TL;
+  i32x4 v[TL::kPer];
+  // p: the tile's first row (KROW) or column at the slice's first contraction
+  // index, ld in bytes, `outer` rows (columns) inside the operand; k0 and kend
+  // in 16-bit units (KROW) or rows from p, row_bytes: length of a KROW row from p
+  __device__ void load(const char* p, int64_t ld, int outer, int k0, int kend, int row_bytes) {
+#pragma unroll
+    for (int u = 0; u < TL::kPer; ++u) {
+      int mr, mc;
+      TL::slot_src(u * 256 + threadIdx.x, 0, k0, mr, mc);
+      const bool row_in = KROW ? mr < outer : mr < kend;
+      const int left = KROW ? min(row_bytes, 2 * kend) - 2 * mc : 2 * (outer - mc);
+      v[u] = i32x4{0, 0, 0, 0};
+      if (!row_in || left <= 0) continue;
+      const char* src = p + (int64_t)mr * ld + 2 * mc;
+      if (left >= 16) {
+        __builtin_memcpy(&v[u], src, 16);
+      } else {
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+          uint32_t x = 0;
+#pragma unroll
+          for (int i = 0; i < 4; i += ES)
+            if (4 * w + i < left)
+              x |= (ES == 2 ? (uint32_t)*reinterpret_cast<const uint16_t*>(src + 4 * w + i)
+                            : (uint32_t)*reinterpret_cast<const uint8_t*>(src + 4 * w + i)) << (8 * i);
+          v[u][w] = (int)x;
+        }
+      }
+    }
+  }
+  __device__ void store(bf16* tile) const {
+#pragma unroll
+    for (int u = 0; u < TL::kPer; ++u) *reinterpret_cast<i32x4*>(tile + 8 * (u * 256 + threadIdx.x)) = v[u];
+  }
+};
+
+// Activation of eight values and its derivative.
+__device__ inline void activate(float (&v)[8], int act) {
+  if (act == kActRelu) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = v[i] < 0.0f ? 0.0f : v[i];
+  } else if (act == kActGelu) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = gelu_f(v[i]);
+  } else if (act == kActSilu) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] *= __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-kLog2e * v[i]));
+  }
+}
+__device__ inline void times_act_grad(float (&d)[8], const float (&t)[8], int act) {
+  if (act == kActRelu) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) d[i] = t[i] > 0.0f ? d[i] : 0.0f;
+  } else if (act == kActGelu) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) d[i] *= gelu_grad_f(t[i]);
+  } else if (act == kActSilu) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float s = __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-kLog2e * t[i]));
+      d[i] *= s * fmaf(t[i], 1.0f - s, 1.0f);
+    }
+  }
+}
+
+// What happens to a sum on its way out.
+struct LinEpi {
+  void *y, *pre;
+  const void* res;
+  const float *bias, *x_scale, *w_scale;
+  int64_t y_ld, pre_ld, res_ld;
+  int act;
+  // float32 sums instead: [slice][M][f_ld]
+  float* outf;
+  int64_t f_ld, f_slice;
+};
+
+// Constants of eight columns.
+struct LinCols {
+  float bias[8], scale[8];
+  __device__ LinCols(const LinEpi& e, int n, int nv) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) { bias[i] = 0.0f; scale[i] = 1.0f; }
+    if (e.bias != nullptr) load8(e.bias + n, nv, bias);
+    if (e.w_scale != nullptr) load8(e.w_scale + n, nv, scale);
+  }
+};
+
+// Columns [n, n + 8) (nv of them inside) of row m.
+template <typename TO>
+__device__ inline void finish8(const LinEpi& e, const LinCols& c, int64_t m, int n, int nv, float (&v)[8]) {
+  if (e.x_scale != nullptr) {
+    const float s = e.x_scale[m];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = fmaf(v[i] * s, c.scale[i], c.bias[i]);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] += c.bias[i];
+  }
+  if (e.pre != nullptr) store8((TO*)e.pre + m * e.pre_ld + n, nv, v);
+  activate(v, e.act);
+  if (e.res != nullptr) {
+    float r[8];
+    load8((const TO*)e.res + m * e.res_ld + n, nv, r);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] += r[i];
+  }
+  store8((TO*)e.y + m * e.y_ld + n, nv, v);
+}
+
+struct GemmArgs {
+  const char *a, *b;       // KROW: [M][K], [N][K]; else [K][M], [K][N]
+  int64_t lda, ldb;        // bytes
+  int64_t M;
+  int N, K;                // K in 16-bit units
+  int kslice;              // units of a contraction slice, whole stages
+  int row_bytes;           // KROW: bytes of a row
+  LinEpi e;
+};
+
+// out[M][N] = sum over k of A(m, k) B(n, k).  The grid holds (slice, tile)
+// pairs; NW 8, 4, or 0: four waves with operands through registers.
+// F32: float32 sums of the slice, else the epilogue.
+template <typename T, typename TO, bool KROW, int NW, bool F32>
+__global__ __launch_bounds__(NW == 8 ? 512 : 256, 1) void lin_gemm_kernel(GemmArgs g) {
+  constexpr int W = NW == 8 ? 8 : 4, NT = W * 64, BM = NW == 8 ? kBM : kBS, BN = BM;
+  constexpr int MI = BM / 64, kWM = 32 * MI;
+  extern __shared__ __align__(16) char smem[];
+  bf16* lds = reinterpret_cast<bf16*>(smem);
+  const int nN = (g.N + BN - 1) / BN;
+  const int tiles = (int)((g.M + BM - 1) / BM) * nN;
+  // Workgroups go to the 8 XCDs in turn; each XCD takes one contiguous run of
+  // (slice, tile) pairs, so that tiles sharing operand rows share an L2.
+  const int total = gridDim.x, xcd = blockIdx.x & 7;
+  const int w0 = xcd * (total >> 3) + min(xcd, total & 7) + (blockIdx.x >> 3);
+  const int z = w0 / tiles, w = w0 - z * tiles;
+  const int tm = w / nN, tn = w - tm * nN;
+  const int64_t m0 = (int64_t)tm * BM;
+  const int n0 = tn * BN;
+  const int kbeg = z * g.kslice, klen = min(g.K - kbeg, g.kslice);
+  const int nk = (klen + kBK - 1) / kBK;
+  const int rows = (int)min((int64_t)BM, g.M - m0), cols = min(BN, g.N - n0);
+  // the tile's operands at the slice's first contraction index
+  const char* pa = g.a + (KROW ? m0 * g.lda + 2 * (int64_t)kbeg : kbeg * g.lda + 2 * m0);
+  const char* pb = g.b + (KROW ? n0 * g.ldb + 2 * (int64_t)kbeg : kbeg * g.ldb + 2 * (int64_t)n0);
+  f32x16 acc[MI][2];
+#pragma unroll
+  for (int i = 0; i < MI; ++i)
+#pragma unroll
+    for (int j = 0; j < 2; ++j) acc[i][j] = f32x16{};
+  if constexpr (NW != 0) {
+    // bytes from the first to the last element of the tile's operand; where the
+    // contraction runs down columns, to the end of that element's 16-byte
+    // chunk (a load that is not wholly inside reads zeros; the chunk starts inside
+    // the operand at a multiple of 16, and what its rest holds reaches only results
+    // outside the output)
+    const uint32_t size_a = (uint32_t)(KROW ? (rows - 1) * g.lda + 2 * klen : (klen - 1) * g.lda + 2 * ((rows + 7) & ~7));
+    const uint32_t size_b = (uint32_t)(KROW ? (cols - 1) * g.ldb + 2 * klen : (klen - 1) * g.ldb + 2 * ((cols + 7) & ~7));
+    const i32x4 rsa = buffer_rsrc(pa, size_a), rsb = buffer_rsrc(pb, size_b);
+    Mat A = {}, B = {};
+    A.ld = (int)(g.lda / 2);
+    B.ld = (int)(g.ldb / 2);
+    typedef Tile<BM, KROW, kBK, NT> TL;
+    Stager<BM, KROW, kBK, NT> sa, sb;
+    sa.init(A, 0, rows, 0);
+    sb.init(B, 0, cols, 0);
+    const int kba = KROW ? 2 : 2 * A.ld, kbb = KROW ? 2 : 2 * B.ld;   // bytes per contraction index
+    constexpr int kRA = NW == 8 ? 3 : 4;
+    auto issue_a = [&](int s, int st) { sa.load(rsa, lds + st * TL::kElems, s * kBK * kba, klen - s * kBK); };
+    auto issue_b = [&](int s, int st) { sb.load(rsb, lds + (kRA + st) * TL::kElems, s * kBK * kbb, klen - s * kBK); };
+    gemm_stages<T, KROW, W>(lds, nk, acc, issue_a, issue_b);
+  } else {
+    typedef Tile<kBS, KROW, kBK, 256> TL;
+    RegStager<KROW, Elem<T>::kBytes> sa, sb;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int wm = (wave / 2) * kWM, wn = (wave % 2) * 64;
+    const int rb = KROW ? g.row_bytes - 2 * kbeg : 0;
+    bf16x8 ao[2][MI], bo[2][2];
+    sa.load(pa, g.lda, rows, 0, klen, rb);
+    sb.load(pb, g.ldb, cols, 0, klen, rb);
+    sa.store(lds);
+    sb.store(lds + TL::kElems);
+    __syncthreads();
+    for (int kt = 0; kt < nk; ++kt) {
+      if (kt + 1 < nk) {
+        sa.load(pa, g.lda, rows, (kt + 1) * kBK, klen, rb);
+        sb.load(pb, g.ldb, cols, (kt + 1) * kBK, klen, rb);
+      }
+      const bf16* ta = lds + 2 * (kt & 1) * TL::kElems;
+      const bf16* tb = ta + TL::kElems;
+#pragma unroll
+      for (int hf = 0; hf < 2; ++hf) {
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+          const int k0 = 32 * hf + 16 * c;
+#pragma unroll
+          for (int j = 0; j < 2; ++j)
+            bo[c][j] = KROW ? row_operand<BN, kBK>(tb, k0, wn + 32 * j, lane) : tr_operand<BN, kBK>(tb, k0, wn + 32 * j, lane);
+#pragma unroll
+          for (int i = 0; i < MI; ++i)
+            ao[c][i] = KROW ? row_operand<BM, kBK>(ta, k0, wm + 32 * i, lane) : tr_operand<BM, kBK>(ta, k0, wm + 32 * i, lane);
+        }
+        stage_products<T>(acc, ao, bo);
+      }
+      if (kt + 1 < nk) {
+        bf16* next = lds + 2 * ((kt + 1) & 1) * TL::kElems;
+        sa.store(next);
+        sb.store(next + TL::kElems);
+      }
+      __syncthreads();
+    }
+  }
+  __syncthreads();   // every wave is done with the stages: their LDS now stages the epilogue
+
+  // 32 rows of the wave's block at a time through its own LDS tile: acc[i][j]
+  // holds rows 32i + 8g + 4h + x (register 4g + x), column 32j + lane % 32;
+  // each lane then handles 8 consecutive columns of rows 8t + lane / 8.
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int wm = (wave / (W / 2)) * kWM, wn = (wave % (W / 2)) * 64;
+  float* et = reinterpret_cast<float*>(smem) + wave * 32 * kEpiS;
+  const int h = lane >> 5, col = lane & 31, er = lane >> 3, ec = (lane & 7) * 8;
+  const int n = n0 + wn + ec, nv = g.N - n;
+  const LinCols lc(F32 ? LinEpi{} : g.e, n, nv);
+#pragma unroll
+  for (int i = 0; i < MI; ++i) {
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) et[(8 * (r / 4) + 4 * h + (r % 4)) * kEpiS + 32 * j + col] = acc[i][j][r];
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+      const int64_t m = m0 + wm + 32 * i + 8 * t + er;
+      float v[8];
+      __builtin_memcpy(v, __builtin_assume_aligned(et + (8 * t + er) * kEpiS + ec, 16), sizeof(v));
+      if (m >= g.M || nv <= 0) continue;
+      if constexpr (F32) store8(g.e.outf + z * g.e.f_slice + m * g.e.f_ld + n, nv, v);
+      else finish8<TO>(g.e, lc, m, n, nv, v);
+    }
+    __builtin_amdgcn_wave_barrier();
+  }
+}
+
+// Contraction slices added in order, then the epilogue (F32: plain float32).
+template <typename TO, bool F32>
+__global__ __launch_bounds__(256) void slices_kernel(const float* __restrict__ part, int ns, int64_t f_slice, int64_t f_ld,
+                                                     int64_t M, int N, LinEpi e) {
+  const int chunks = (N + 7) / 8;
+  const int64_t idx = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (idx >= M * chunks) return;
+  const int64_t m = idx / chunks;
+  const int n = 8 * (int)(idx - m * chunks);
+  float v[8] = {};
+  for (int s = 0; s < ns; ++s) {
+    float p[8];
+    __builtin_memcpy(p, __builtin_assume_aligned(part + s * f_slice + m * f_ld + n, 16), sizeof(p));
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] += p[i];
+  }
+  if constexpr (F32) {
+    store8(e.outf + m * e.f_ld + n, N - n, v);
+  } else {
+    const LinCols lc(e, n, N - n);
+    finish8<TO>(e, lc, m, n, N - n, v);
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Few tokens: what counts is to read W once at the rate of the HBM.  A
+// workgroup takes 16 RT rows of W (columns of y) and up to 16 MT tokens; its
+// waves take 128-byte pieces of the rows in turn, straight from memory in the
+// layout of the 16 x 16 matrix instruction (W the A operand, x the B operand:
+// lane l holds row l % 16, bytes 16 (l / 16) and 64 further on), and their sums
+// are added through LDS in wave order.  No barrier stands between the loads.
+// ---------------------------------------------------------------------------
+typedef _Float16 half8 __attribute__((ext_vector_type(8)));
+
+template <typename T>
+__device__ inline void skinny_mma(f32x4& acc, const i32x4 (&a)[2], const i32x4 (&b)[2]) {
+  if constexpr (std::is_same<T, e4m3>::value) {
+    const i32x8 x = {a[0][0], a[0][1], a[0][2], a[0][3], a[1][0], a[1][1], a[1][2], a[1][3]};
+    const i32x8 y = {b[0][0], b[0][1], b[0][2], b[0][3], b[1][0], b[1][1], b[1][2], b[1][3]};
+    acc = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(x, y, acc, 0, 0, 0, kUnitScale, 0, kUnitScale);
+  } else {
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      if constexpr (std::is_same<T, __bf16>::value)
+        acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a[j]), __builtin_bit_cast(bf16x8, b[j]), acc, 0, 0, 0);
+      else
+        acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a[j]), __builtin_bit_cast(f16x8, b[j]), acc, 0, 0, 0);
+    }
+  }
+}
+
+// Up to 16 bytes of a row, `left` of them inside it, the rest zero.
+template <int ES>
+__device__ inline i32x4 row_tail(const char* p, int left) {
+  i32x4 v = {0, 0, 0, 0};
+  if (left >= 16) {
+    __builtin_memcpy(&v, p, 16);
+    return v;
+  }
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    uint32_t x = 0;
+#pragma unroll
+    for (int i = 0; i < 4; i += ES)
+      if (4 * w + i < left)
+        x |= (ES == 2 ? (uint32_t)*reinterpret_cast<const uint16_t*>(p + 4 * w + i)
+                      : (uint32_t)*reinterpret_cast<const uint8_t*>(p + 4 * w + i)) << (8 * i);
+    v[w] = (int)x;
+  }
+  return v;
+}
+
+struct SkinnyArgs {
+  const char *x, *w;
+  int64_t ldx, ldw;        // bytes
+  int M, N, row_bytes;
+  LinEpi e;
+};
+
+constexpr int kSkinnyMost = 64;    // tokens
+constexpr int kRedS = 20;          // stride (floats) of a token's 16 columns in the joining LDS
+
+template <typename T, typename TO, int MT, int RT>
+__global__ __launch_bounds__(1024) void skinny_kernel(SkinnyArgs g) {
+  constexpr int ES = Elem<T>::kBytes;
+  extern __shared__ __align__(16) float red[];      // [wave][MT][RT][16 tokens][kRedS]
+  const int lane = threadIdx.x & 63, waves = blockDim.x >> 6;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int r = lane & 15, q = lane >> 4;
+  const int n0 = blockIdx.x * 16 * RT;
+  const char* pw[RT];
+  const char* px[MT];
+  // rows past the end repeat the last one; their results are dropped
+#pragma unroll
+  for (int i = 0; i < RT; ++i) pw[i] = g.w + (int64_t)min(n0 + 16 * i + r, g.N - 1) * g.ldw + 16 * q;
+#pragma unroll
+  for (int i = 0; i < MT; ++i) px[i] = g.x + (int64_t)min(16 * i + r, g.M - 1) * g.ldx + 16 * q;
+  f32x4 acc[MT][RT];
+#pragma unroll
+  for (int i = 0; i < MT; ++i)
+#pragma unroll
+    for (int j = 0; j < RT; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+  const int full = g.row_bytes >> 7;
+  // U pieces at a time, so that their loads go out together
+  constexpr int U = MT + RT <= 2 ? 4 : MT + RT <= 4 ? 2 : 1;
+  auto pieces = [&](int it, auto count) {
+    constexpr int C = decltype(count)::value;
+    i32x4 a[C][RT][2], b[C][MT][2];
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      const int64_t o = (int64_t)(it + c * waves) << 7;
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+#pragma unroll
+        for (int i = 0; i < RT; ++i) __builtin_memcpy(&a[c][i][j], pw[i] + o + 64 * j, 16);
+#pragma unroll
+        for (int i = 0; i < MT; ++i) __builtin_memcpy(&b[c][i][j], px[i] + o + 64 * j, 16);
+      }
+    }
+#pragma unroll
+    for (int c = 0; c < C; ++c)
+#pragma unroll
+      for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int j = 0; j < RT; ++j) skinny_mma<T>(acc[i][j], a[c][j], b[c][i]);
+  };
+  int it = wave;
+  for (; it + (U - 1) * waves < full; it += U * waves) pieces(it, std::integral_constant<int, U>{});
+  for (; it < full; it += waves) pieces(it, std::integral_constant<int, 1>{});
+  if ((g.row_bytes & 127) != 0 && wave == full % waves) {
+    i32x4 a[RT][2], b[MT][2];
+    const int64_t o = (int64_t)full << 7;
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      const int left = g.row_bytes - (full << 7) - 16 * q - 64 * j;
+#pragma unroll
+      for (int i = 0; i < RT; ++i) a[i][j] = row_tail<ES>(pw[i] + o + 64 * j, left);
+#pragma unroll
+      for (int i = 0; i < MT; ++i) b[i][j] = row_tail<ES>(px[i] + o + 64 * j, left);
+    }
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+      for (int j = 0; j < RT; ++j) skinny_mma<T>(acc[i][j], a[j], b[i]);
+  }
+  // lane (r, q) holds columns 4 q .. 4 q + 3 of token r
+#pragma unroll
+  for (int i = 0; i < MT; ++i)
+#pragma unroll
+    for (int j = 0; j < RT; ++j)
+      *reinterpret_cast<f32x4*>(red + ((wave * MT + i) * RT + j) * 16 * kRedS + r * kRedS + 4 * q) = acc[i][j];
+  __syncthreads();
+  // eight columns a thread
+  for (int idx = threadIdx.x; idx < MT * RT * 32; idx += blockDim.x) {
+    const int half = idx & 1, j = (idx >> 1) % RT, tok = (idx >> 1) / RT;
+    const int n = n0 + 16 * j + 8 * half, nv = g.N - n;
+    if (tok >= g.M || nv <= 0) continue;
+    float v[8] = {};
+    for (int w = 0; w < waves; ++w) {
+      const float* p = red + ((w * MT + (tok >> 4)) * RT + j) * 16 * kRedS + (tok & 15) * kRedS + 8 * half;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] += p[i];
+    }
+    const LinCols lc(g.e, n, nv);
+    finish8<TO>(g.e, lc, tok, n, nv, v);
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Backward: dt = dy act'(pre), dx = dt W, dW = dt^T x, dbias = sum of dt's rows.
+// ---------------------------------------------------------------------------
+
+// dt rounded to the operands' type, with rows of whole 16-byte chunks (zeros
+// behind the last column), and the column sums of the float32 dt over each of
+// gridDim.y runs of rows.  32 threads along 256 columns, eight rows at a time.
+template <typename T>
+__global__ __launch_bounds__(256) void act_grad_kernel(const T* __restrict__ dy, int64_t dy_ld, const T* __restrict__ pre,
+                                                       int64_t pre_ld, T* __restrict__ dt, int64_t dt_ld,
+                                                       float* __restrict__ part, int64_t M, int N, int64_t run, int act) {
+  __shared__ float red[8][32][9];
+  const int c = threadIdx.x & 31, r = threadIdx.x >> 5;
+  const int n = 256 * blockIdx.x + 8 * c, nv = N - n;
+  const int64_t end = min(M, (blockIdx.y + 1) * run);
+  float s[8] = {};
+  if (nv > 0) {
+    for (int64_t m = blockIdx.y * run + r; m < end; m += 8) {
+      float d[8], t[8];
+      load8(dy + m * dy_ld + n, nv, d);
+      if (act != kActNone) {
+        load8(pre + m * pre_ld + n, nv, t);
+        times_act_grad(d, t, act);
+        if (nv < 8)
+#pragma unroll
+          for (int i = 0; i < 8; ++i) d[i] = i < nv ? d[i] : 0.0f;
+      }
+#pragma unroll
+      for (int i = 0; i < 8; ++i) s[i] += d[i];
+      if (dt != nullptr) store8(dt + m * dt_ld + n, 8, d);
+    }
+  }
+  if (part == nullptr) return;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) red[r][c][i] = s[i];
+  __syncthreads();
+  const int col = threadIdx.x;               // of the workgroup's 256
+  float sum = 0.0f;
+#pragma unroll
+  for (int k = 0; k < 8; ++k) sum += red[k][col >> 3][col & 7];
+  if (256 * blockIdx.x + col < N) part[(int64_t)blockIdx.y * N + 256 * blockIdx.x + col] = sum;
+}
+
+// out[k][n] = w[n][k] of an N x K matrix, rows of out of whole 16-byte chunks
+// with zeros behind the last column: the data gradient's operand, contracted
+// along memory rows.  64 x 64 tiles.
+template <typename T>
+__global__ __launch_bounds__(256) void transpose_kernel(const T* __restrict__ w, int64_t w_ld, T* __restrict__ out, int64_t out_ld,
+                                                        int N, int K) {
+  __shared__ T tile[64][66];
+  const int n0 = 64 * blockIdx.y, k0 = 64 * blockIdx.x;
+#pragma unroll
+  for (int u = 0; u < 2; ++u) {
+    const int r = (threadIdx.x >> 3) + 32 * u, c = 8 * (threadIdx.x & 7);
+    float v[8] = {};
+    if (n0 + r < N) load8(w + (int64_t)(n0 + r) * w_ld + k0 + c, K - k0 - c, v);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) tile[r][c + i] = from_float<T>(v[i]);
+  }
+  __syncthreads();
+#pragma unroll
+  for (int u = 0; u < 2; ++u) {
+    const int k = (threadIdx.x >> 3) + 32 * u, c = 8 * (threadIdx.x & 7);
+    if (k0 + k >= K || n0 + c >= out_ld) continue;
+    float v[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = to_float<T>(tile[c + i][k]);
+    store8(out + (int64_t)(k0 + k) * out_ld + n0 + c, 8, v);
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Host side.
+// ---------------------------------------------------------------------------
+constexpr int kCus = 256;          // compute units the plans are made for
+constexpr int kMaxSplit = 8;       // contraction slices of a forward product
+constexpr int kMaxTokenSlices = 64;
+constexpr int kMaxRuns = 512;      // runs of rows of the column sums
+
+int64_t up8(int64_t n) { return (n + 7) / 8 * 8; }
+size_t al(size_t n) { return (n + 255) / 256 * 256; }
+int slice_len(int K, int ns) { return ((K + ns - 1) / ns + kBK - 1) / kBK * kBK; }
+
+// Waves of a workgroup (8: 256 x 256 tiles, 4: 128 x 128) and contraction
+// slices, by the time of the slowest compute unit, in us: a stage of 64 units
+// takes 1.35 with eight waves, 0.65 with four, a workgroup 8 and 3 besides; a
+// sum of slices 5 and its traffic.
+struct Plan {
+  int nw, ns;
+};
+double plan_cost(int64_t M, int N, int K, Plan p) {
+  const int bm = p.nw == 8 ? kBM : kBS;
+  const double tiles = (double)((M + bm - 1) / bm) * ((N + bm - 1) / bm);
+  const double rounds = (double)(int64_t)((tiles * p.ns + kCus - 1) / kCus);
+  const int stages = slice_len(K, p.ns) / kBK;
+  const double sum = p.ns > 1 ? 5.0 + 2e-6 * p.ns * M * N : 0.0;
+  return rounds * (p.nw == 8 ? 1.35 * stages + 8.0 : 0.65 * stages + 3.0) + sum;
+}
+Plan plan_product(int64_t M, int N, int K, int most, bool eight) {
+  Plan best = {eight ? 8 : 4, 1};
+  double c = plan_cost(M, N, K, best);
+  for (int ns = 1; ns <= most && (ns == 1 || K >= 4 * kBK * ns); ++ns) {
+    const double d = plan_cost(M, N, K, {4, ns});
+    if (d < c) { c = d; best = {4, ns}; }
+  }
+  const int len = slice_len(K, best.ns);
+  best.ns = (K + len - 1) / len;             // none past the end
+  return best;
+}
+// A weight gradient over T tokens: token slices for two whole rounds of the
+// eight-wave form, or what the four-wave form does in fewer.
+Plan plan_wgrad(int64_t T, int N, int K, bool eight) {
+  const int Ti = (int)std::max<int64_t>(T, 1);
+  Plan best = plan_product(N, K, Ti, kMaxSplit, false);
+  if (eight) {
+    const int64_t tiles = (int64_t)((N + kBM - 1) / kBM) * ((K + kBM - 1) / kBM);
+    int64_t n = std::max<int64_t>(1, 2 * kCus / tiles);
+    n = std::min(n, std::max<int64_t>(1, T / (4 * kBK)));
+    n = std::min<int64_t>(n, kMaxTokenSlices);
+    const Plan p = {8, (int)n};
+    if (plan_cost(N, K, Ti, p) <= plan_cost(N, K, Ti, best)) best = p;
+  }
+  const int len = slice_len(Ti, best.ns);
+  best.ns = (Ti + len - 1) / len;
+  return best;
+}
+
+template <typename T, typename TO, bool KROW, int NW, bool F32>
+hipError_t gemm_launch(GemmArgs g, int ns, hipStream_t st) {
+  constexpr int BM = NW == 8 ? kBM : kBS;
+  // stages of A and B: 3 + 2 of 32 KB, 4 + 4 of 16 KB, or 2 + 2 of 16 KB
+  constexpr size_t lds = (NW == 8 ? 5 : NW == 4 ? 8 : 4) * (size_t)BM * kBK * 2;
+  const int64_t tiles = (g.M + BM - 1) / BM * ((g.N + BM - 1) / BM);
+  g.kslice = slice_len(g.K, ns);
+  hipLaunchKernelGGL((lin_gemm_kernel<T, TO, KROW, NW, F32>), dim3((unsigned)(tiles * ns)), dim3(NW == 8 ? 512 : 256), lds, st, g);
+  return hipGetLastError();
+}
+
+// What the direct-to-LDS loads take: rows of 16-byte chunks at 16-byte places,
+// and `rows` of them (a tile's, or a slice's) within 2^31 bytes.
+bool direct_ok(const void* p, int64_t ld_bytes, int64_t rows) {
+  return ((uintptr_t)p | (uint64_t)ld_bytes) % 16 == 0 && rows * ld_bytes < ((int64_t)1 << 31);
+}
+
+// One product of plan p: slices into `part` and their sum, or straight through
+// the epilogue.
+template <typename T, typename TO, bool KROW>
+hipError_t product_form(const GemmArgs& g, Plan p, bool direct, bool f32, float* part, hipStream_t st) {
+  GemmArgs s = g;
+  if (p.ns > 1) {
+    s.e.outf = part;
+    s.e.f_ld = up8(g.N);
+    s.e.f_slice = g.M * s.e.f_ld;
+  }
+  hipError_t e;
+  if (f32 || p.ns > 1) {
+    if constexpr (!KROW) {
+      e = !direct ? gemm_launch<T, TO, KROW, 0, true>(s, p.ns, st)
+          : p.nw == 8 ? gemm_launch<T, TO, KROW, 8, true>(s, p.ns, st)
+                      : gemm_launch<T, TO, KROW, 4, true>(s, p.ns, st);
+    } else {
+      // forward slices are taken by the four-wave forms only
+      e = direct ? gemm_launch<T, TO, KROW, 4, true>(s, p.ns, st) : gemm_launch<T, TO, KROW, 0, true>(s, p.ns, st);
+    }
+  } else {
+    e = !direct ? gemm_launch<T, TO, KROW, 0, false>(s, 1, st)
+        : p.nw == 8 ? gemm_launch<T, TO, KROW, 8, false>(s, 1, st)
+                    : gemm_launch<T, TO, KROW, 4, false>(s, 1, st);
+  }
+  if (e != hipSuccess || p.ns == 1) return e;
+  const int64_t n = g.M * ((g.N + 7) / 8);
+  const dim3 grid((unsigned)((n + 255) / 256));
+  if (f32) hipLaunchKernelGGL((slices_kernel<TO, true>), grid, dim3(256), 0, st, part, p.ns, s.e.f_slice, s.e.f_ld, g.M, g.N, g.e);
+  else hipLaunchKernelGGL((slices_kernel<TO, false>), grid, dim3(256), 0, st, part, p.ns, s.e.f_slice, s.e.f_ld, g.M, g.N, g.e);
+  return hipGetLastError();
+}
+
+template <typename TO>
+void skip_rows(GemmArgs& g, int64_t rows) {
+  g.a += rows * g.lda;
+  g.M -= rows;
+  LinEpi& e = g.e;
+  e.y = (TO*)e.y + rows * e.y_ld;
+  if (e.pre != nullptr) e.pre = (TO*)e.pre + rows * e.pre_ld;
+  if (e.res != nullptr) e.res = (const TO*)e.res + rows * e.res_ld;
+  if (e.x_scale != nullptr) e.x_scale += rows;
+}
+
+// A product along memory rows: few tiles by plan_product; many as the rows of
+// whole rounds of one 256 x 256 tile a compute unit, and the rest by itself.
+template <typename T, typename TO>
+hipError_t row_product(GemmArgs g, float* part, hipStream_t st) {
+  const bool direct = direct_ok(g.a, g.lda, kBM) && direct_ok(g.b, g.ldb, kBM) && g.row_bytes % 16 == 0;
+  Plan p = plan_product(g.M, g.N, g.K, kMaxSplit, direct);
+  if (p.nw == 8) {
+    const int64_t nN = (g.N + kBM - 1) / kBM, nM = (g.M + kBM - 1) / kBM;
+    const int64_t whole = nM * nN / kCus * kCus / nN;       // row tiles in whole rounds
+    if (whole > 0 && whole < nM) {
+      GemmArgs first = g;
+      first.M = whole * kBM;
+      const hipError_t e = product_form<T, TO, true>(first, Plan{8, 1}, true, false, nullptr, st);
+      if (e != hipSuccess) return e;
+      skip_rows<TO>(g, first.M);
+      p = plan_product(g.M, g.N, g.K, 1, true);
+    }
+  }
+  return product_form<T, TO, true>(g, p, direct, false, part, st);
+}
+
+template <typename T, typename TO, int MT>
+hipError_t skinny_rt(const SkinnyArgs& g, hipStream_t st) {
+  const int its = (g.row_bytes + 127) / 128;
+  const int rt = (g.N + 15) / 16 >= 4 * kCus ? 2 : 1;
+  int waves = 16;
+  while (waves > 1 && waves * 2 > its) waves /= 2;
+  const dim3 grid((g.N + 16 * rt - 1) / (16 * rt));
+  const size_t lds = (size_t)waves * MT * rt * 16 * kRedS * sizeof(float);
+  if (rt == 2) hipLaunchKernelGGL((skinny_kernel<T, TO, MT, 2>), grid, dim3(64 * waves), lds, st, g);
+  else hipLaunchKernelGGL((skinny_kernel<T, TO, MT, 1>), grid, dim3(64 * waves), lds, st, g);
+  return hipGetLastError();
+}
+
+template <typename T, typename TO>
+hipError_t fwd_t(const LinFwd& a, void* ws, hipStream_t st) {
+  constexpr int ES = Elem<T>::kBytes;
+  LinEpi e = {};
+  e.y = a.y; e.pre = a.pre; e.res = a.res; e.bias = a.bias; e.x_scale = a.x_scale; e.w_scale = a.w_scale;
+  e.y_ld = a.y_ld; e.pre_ld = a.pre_ld; e.res_ld = a.res_ld; e.act = a.act;
+  if (a.M <= kSkinnyMost) {
+    SkinnyArgs g = {(const char*)a.x, (const char*)a.w, a.x_ld * ES, a.w_ld * ES, (int)a.M, a.N, a.K * ES, e};
+    return a.M <= 16 ? skinny_rt<T, TO, 1>(g, st) : a.M <= 32 ? skinny_rt<T, TO, 2>(g, st) : skinny_rt<T, TO, 4>(g, st);
+  }
+  GemmArgs g = {};
+  g.a = (const char*)a.x; g.b = (const char*)a.w; g.lda = a.x_ld * ES; g.ldb = a.w_ld * ES;
+  g.M = a.M; g.N = a.N; g.row_bytes = a.K * ES; g.K = (g.row_bytes + 1) / 2; g.e = e;
+  return row_product<T, TO>(g, (float*)ws, st);
+}
+
+// Backward workspace: dt, the transposed W, slices of either product, column sums.
+struct BwdWs {
+  size_t dt, wt, part, sums, total;
+  int64_t dt_ld, run;
+  int runs;
+};
+size_t split_floats(int64_t M, int N, int K, bool eight) {
+  const Plan p = plan_product(M, N, K, kMaxSplit, eight);
+  return p.ns > 1 ? (size_t)p.ns * M * up8(N) : 0;
+}
+BwdWs bwd_ws(int64_t M, int N, int K) {
+  BwdWs w;
+  w.dt_ld = up8(N);
+  w.runs = (int)std::min<int64_t>(kMaxRuns, std::max<int64_t>(1, (M + 63) / 64));
+  w.run = (M + w.runs - 1) / w.runs;
+  size_t part = 0;
+  for (bool eight : {false, true}) {
+    part = std::max(part, split_floats(M, K, (int)w.dt_ld, eight));
+    const Plan p = plan_wgrad(M, N, K, eight);
+    if (p.ns > 1) part = std::max(part, (size_t)p.ns * N * up8(K));
+  }
+  size_t off = 0;
+  w.dt = off; off += al((size_t)M * w.dt_ld * 2);
+  w.wt = off; off += al((size_t)K * w.dt_ld * 2);
+  w.part = off; off += al(part * 4);
+  w.sums = off; off += al((size_t)w.runs * N * 4);
+  w.total = off;
+  return w;
+}
+
+template <typename T>
+hipError_t bwd_t(const LinBwd& a, char* ws, hipStream_t st) {
+  const BwdWs w = bwd_ws(a.M, a.N, a.K);
+  hipError_t e;
+  const bool need_dt = (a.dx != nullptr || a.dw != nullptr) &&
+                       (a.act != kActNone || a.N % 8 != 0 || !direct_ok(a.dy, a.dy_ld * 2, kBM));
+  T* dt = need_dt ? (T*)(ws + w.dt) : nullptr;
+  float* sums = a.db != nullptr ? (float*)(ws + w.sums) : nullptr;
+  if (need_dt || sums != nullptr) {
+    hipLaunchKernelGGL((act_grad_kernel<T>), dim3((a.N + 255) / 256, w.runs), dim3(256), 0, st, (const T*)a.dy, a.dy_ld,
+                       (const T*)a.pre, a.pre_ld, dt, w.dt_ld, sums, a.M, a.N, w.run, a.act);
+    if ((e = hipGetLastError()) != hipSuccess) return e;
+  }
+  if (sums != nullptr && (e = launch_part_sum(sums, a.db, w.runs, a.N, st)) != hipSuccess) return e;
+  const char* d = need_dt ? (const char*)dt : (const char*)a.dy;
+  const int64_t d_ld = 2 * (need_dt ? w.dt_ld : a.dy_ld);
+  float* part = (float*)(ws + w.part);
+  if (a.dx != nullptr && a.M > 0) {
+    T* wt = (T*)(ws + w.wt);
+    hipLaunchKernelGGL((transpose_kernel<T>), dim3((a.K + 63) / 64, (unsigned)((w.dt_ld + 63) / 64)), dim3(256), 0, st, (const T*)a.w,
+                       a.w_ld, wt, w.dt_ld, a.N, a.K);
+    if ((e = hipGetLastError()) != hipSuccess) return e;
+    GemmArgs g = {};
+    g.a = d; g.lda = d_ld; g.b = (const char*)wt; g.ldb = 2 * w.dt_ld;
+    g.M = a.M; g.N = a.K; g.K = (int)w.dt_ld; g.row_bytes = 2 * (int)w.dt_ld;
+    g.e.y = a.dx; g.e.y_ld = a.dx_ld;
+    if ((e = row_product<T, T>(g, part, st)) != hipSuccess) return e;
+  }
+  if (a.dw != nullptr) {
+    GemmArgs g = {};
+    g.a = d; g.lda = d_ld; g.b = (const char*)a.x; g.ldb = 2 * a.x_ld;
+    g.M = a.N; g.N = a.K; g.K = (int)a.M;
+    if (a.dw_f32) { g.e.outf = (float*)a.dw; g.e.f_ld = a.dw_ld; }
+    else { g.e.y = a.dw; g.e.y_ld = a.dw_ld; }
+    Plan p = plan_wgrad(a.M, a.N, a.K, true);
+    const int64_t rows = slice_len(g.K, p.ns);
+    const bool direct = direct_ok(g.a, g.lda, rows) && direct_ok(g.b, g.ldb, rows);
+    if (!direct) p = plan_wgrad(a.M, a.N, a.K, false);
+    if ((e = product_form<T, T, false>(g, p, direct, a.dw_f32, part, st)) != hipSuccess) return e;
+  }
+  return hipSuccess;
+}
+
+}  // namespace
+
+size_t lin_fwd_workspace(int64_t M, int N, int K, int dtype) {
+  if (M <= kSkinnyMost) return 0;
+  const int ku = dtype == kE4m3 ? (K + 1) / 2 : K;
+  return 4 * std::max(split_floats(M, N, ku, true), split_floats(M, N, ku, false));
+}
+size_t lin_bwd_workspace(int64_t M, int N, int K) { return bwd_ws(M, N, K).total; }
+
+hipError_t launch_lin_fwd(int dtype, int out, const LinFwd& a, void* ws, hipStream_t st) {
+  if (a.M == 0) return hipSuccess;
+  if (dtype == kBf16) return fwd_t<__bf16, __bf16>(a, ws, st);
+  if (dtype == kF16) return fwd_t<_Float16, _Float16>(a, ws, st);
+  return out == kBf16 ? fwd_t<e4m3, __bf16>(a, ws, st) : fwd_t<e4m3, _Float16>(a, ws, st);
+}
+
+hipError_t launch_lin_bwd(int dtype, const LinBwd& a, void* ws, hipStream_t st) {
+  return dtype == kBf16 ? bwd_t<__bf16>(a, (char*)ws, st) : bwd_t<_Float16>(a, (char*)ws, st);
+}
+
+}  // namespace terra

@@ -1,0 +1,455 @@
+// norm.hip - root-mean-square norm with the residual's addition, forward (in
+// the element type or in e4m3 with one scale a row) and backward.
+//
+//   z = x + res,  rstd = 1 / sqrt(mean(z^2) + eps),  y = gain z rstd
+//   q = e4m3(y / s),  s = max(max |y| / 448, 2^-126)
+// z, its squares and y stay in float32; every output is rounded once, z too:
+// the norm is that of the sum before z is rounded.  Backward, with
+// zh = z rstd and g = dy gain, the stored z and dz the gradient that reaches z
+// by the residual stream:
+//   dx = rstd (g - zh mean(g zh)) + dz,   dgain = sum over rows of dy zh
+// dx is the gradient of x and of res alike.
+//
+// What bounds it: HBM, a row is read once and stays in registers.  A row is
+// held by TPR threads (one wave, 256 or 1024 threads), thread t with the
+// 8-element chunks t, t + TPR, ... (NCH of them).
+#include "terra_vec.h"
+#include "terra_ops.h"
+
+namespace terra {
+
+namespace {
+
+// Sum and maximum over a wave, in every lane.
+__device__ inline float lanes_sum(float x) {
+#pragma unroll
+  for (int o = 32; o >= 1; o >>= 1) x += __shfl_xor(x, o, 64);
+  return x;
+}
+__device__ inline uint32_t lanes_max(uint32_t x) {
+#pragma unroll
+  for (int o = 32; o >= 1; o >>= 1) x = max(x, (uint32_t)__shfl_xor((int)x, o, 64));
+  return x;
+}
+
+// The same over the threads that hold one row.  `red` has a slot for each
+// wave; the waves' values are added in order.
+template <int TPR>
+__device__ inline float row_sum(float x, float* red) {
+  x = lanes_sum(x);
+  if (TPR == 64) return x;
+  __syncthreads();                       // the last use of red is over
+  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = x;
+  __syncthreads();
+  float s = 0.0f;
+#pragma unroll
+  for (int w = 0; w < TPR / 64; ++w) s += red[w];
+  return s;
+}
+// Magnitudes as their bits: their order is that of the numbers, infinity above
+// them and NaN above infinity, so that a NaN is not lost.
+template <int TPR>
+__device__ inline uint32_t row_max(uint32_t x, float* red) {
+  x = lanes_max(x);
+  if (TPR == 64) return x;
+  uint32_t* r = reinterpret_cast<uint32_t*>(red);
+  __syncthreads();
+  if ((threadIdx.x & 63) == 0) r[threadIdx.x >> 6] = x;
+  __syncthreads();
+  uint32_t s = 0;
+#pragma unroll
+  for (int w = 0; w < TPR / 64; ++w) s = max(s, r[w]);
+  return s;
+}
+__device__ inline uint32_t mag(float x) { return __float_as_uint(x) & 0x7fffffffu; }
+
+// Scale of a row in e4m3 from the bits of its largest magnitude (a NaN stays
+// one: the maximum would drop it).
+__device__ inline float e4m3_scale(uint32_t amax) {
+  const float s = __uint_as_float(amax) / kE4m3Max;
+  return s < 1.17549435e-38f ? 1.17549435e-38f : s;
+}
+
+template <int TPR>
+struct Rows {
+  static constexpr int kThreads = TPR == 64 ? 256 : TPR;
+  static constexpr int kPer = kThreads / TPR;     // rows of a workgroup at a time
+};
+
+template <typename T, int TPR, int NCH>
+__global__ __launch_bounds__(Rows<TPR>::kThreads) void rms_fwd_kernel(RmsFwd a) {
+  __shared__ float red[16];
+  const T* X = (const T*)a.x;
+  const T* R = (const T*)a.res;
+  T* Z = (T*)a.z;
+  T* Y = (T*)a.y;
+  const int t = threadIdx.x % TPR;
+  const int64_t step = (int64_t)gridDim.x * Rows<TPR>::kPer;
+  float g[NCH][8];
+#pragma unroll
+  for (int c = 0; c < NCH; ++c) {
+    const int col = 8 * (t + TPR * c);
+    if (a.gain != nullptr) load8(a.gain + col, a.cols - col, g[c]);
+    else
+#pragma unroll
+      for (int i = 0; i < 8; ++i) g[c][i] = 1.0f;
+  }
+  for (int64_t row = (int64_t)blockIdx.x * Rows<TPR>::kPer + threadIdx.x / TPR; row < a.rows; row += step) {
+    float z[NCH][8];
+#pragma unroll
+    for (int c = 0; c < NCH; ++c) {
+      const int col = 8 * (t + TPR * c);
+      load8(X + row * a.x_ld + col, a.cols - col, z[c]);
+    }
+    if (R != nullptr) {
+#pragma unroll
+      for (int c = 0; c < NCH; ++c) {
+        const int col = 8 * (t + TPR * c);
+        float r[8];
+        load8(R + row * a.res_ld + col, a.cols - col, r);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) z[c][i] += r[i];
+      }
+    }
+    float ss = 0.0f;
+#pragma unroll
+    for (int c = 0; c < NCH; ++c)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) ss = fmaf(z[c][i], z[c][i], ss);
+    if (Z != nullptr) {
+#pragma unroll
+      for (int c = 0; c < NCH; ++c) {
+        const int col = 8 * (t + TPR * c);
+        store8(Z + row * a.z_ld + col, a.cols - col, z[c]);
+      }
+    }
+    const float rstd = 1.0f / sqrtf(row_sum<TPR>(ss, red) / (float)a.cols + a.eps);
+    if (a.rstd != nullptr && t == 0) a.rstd[row] = rstd;
+    uint32_t amax = 0;
+#pragma unroll
+    for (int c = 0; c < NCH; ++c)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        z[c][i] = z[c][i] * rstd * g[c][i];
+        amax = max(amax, mag(z[c][i]));
+      }
+    if (Y != nullptr) {
+#pragma unroll
+      for (int c = 0; c < NCH; ++c) {
+        const int col = 8 * (t + TPR * c);
+        store8(Y + row * a.y_ld + col, a.cols - col, z[c]);
+      }
+    }
+    if (a.q != nullptr) {
+      const float s = e4m3_scale(row_max<TPR>(amax, red));
+      if (t == 0) a.q_scale[row] = s;
+      const float inv = 1.0f / s;
+#pragma unroll
+      for (int c = 0; c < NCH; ++c) {
+        const int col = 8 * (t + TPR * c);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) z[c][i] *= inv;
+        store8_e4m3(a.q + row * a.q_ld + col, a.cols - col, z[c]);
+      }
+    }
+  }
+}
+
+// Rows longer than the registers of a workgroup: read twice, the second time
+// from the L2.  Only the second pass writes, so that outputs in place of an
+// input are not read again.
+template <typename T>
+__global__ __launch_bounds__(1024) void rms_fwd_long_kernel(RmsFwd a) {
+  __shared__ float red[16];
+  const T* X = (const T*)a.x;
+  const T* R = (const T*)a.res;
+  T* Z = (T*)a.z;
+  T* Y = (T*)a.y;
+  auto load = [&](int64_t row, int col, float (&z)[8], float (&g)[8]) {
+    load8(X + row * a.x_ld + col, a.cols - col, z);
+    if (R != nullptr) {
+      load8(R + row * a.res_ld + col, a.cols - col, g);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) z[i] += g[i];
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) g[i] = 1.0f;
+    if (a.gain != nullptr) load8(a.gain + col, a.cols - col, g);
+  };
+  for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
+    float ss = 0.0f;
+    uint32_t amax = 0;
+    for (int col = 8 * threadIdx.x; col < a.cols; col += 8192) {
+      float z[8], g[8];
+      load(row, col, z, g);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        ss = fmaf(z[i], z[i], ss);
+        amax = max(amax, mag(z[i] * g[i]));
+      }
+    }
+    const float rstd = 1.0f / sqrtf(row_sum<1024>(ss, red) / (float)a.cols + a.eps);
+    float inv = 0.0f;
+    if (a.q != nullptr) {
+      const float m = __uint_as_float(row_max<1024>(amax, red)) * rstd;
+      const float s = e4m3_scale(mag(m));
+      inv = 1.0f / s;
+      if (threadIdx.x == 0) a.q_scale[row] = s;
+    }
+    if (a.rstd != nullptr && threadIdx.x == 0) a.rstd[row] = rstd;
+    for (int col = 8 * threadIdx.x; col < a.cols; col += 8192) {
+      float z[8], g[8];
+      load(row, col, z, g);
+      if (Z != nullptr) store8(Z + row * a.z_ld + col, a.cols - col, z);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) z[i] = z[i] * rstd * g[i];
+      if (Y != nullptr) store8(Y + row * a.y_ld + col, a.cols - col, z);
+      if (a.q != nullptr) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) z[i] *= inv;
+        store8_e4m3(a.q + row * a.q_ld + col, a.cols - col, z);
+      }
+    }
+  }
+}
+
+// Backward.  Each wave (or workgroup) walks the rows one grid apart and keeps
+// its share of dgain in registers; the waves of a workgroup add theirs in
+// order through LDS, and the workgroup leaves one row of `part`.
+template <typename T, int TPR, int NCH>
+__global__ __launch_bounds__(Rows<TPR>::kThreads) void rms_bwd_kernel(RmsBwd a) {
+  constexpr int kPer = Rows<TPR>::kPer;
+  __shared__ float red[16];
+  __shared__ float joint[TPR == 64 ? 8 * TPR * NCH : 1];
+  const T* DY = (const T*)a.dy;
+  const T* Z = (const T*)a.z;
+  const T* DZ = (const T*)a.dz;
+  T* DX = (T*)a.dx;
+  const int t = threadIdx.x % TPR;
+  const int64_t step = (int64_t)gridDim.x * kPer;
+  float g[NCH][8], dg[NCH][8];
+#pragma unroll
+  for (int c = 0; c < NCH; ++c) {
+    const int col = 8 * (t + TPR * c);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) { g[c][i] = 1.0f; dg[c][i] = 0.0f; }
+    if (a.gain != nullptr) load8(a.gain + col, a.cols - col, g[c]);
+  }
+  const float inv = 1.0f / (float)a.cols;
+  for (int64_t row = (int64_t)blockIdx.x * kPer + threadIdx.x / TPR; row < a.rows; row += step) {
+    float d[NCH][8], zh[NCH][8];
+#pragma unroll
+    for (int c = 0; c < NCH; ++c) {
+      const int col = 8 * (t + TPR * c);
+      load8(DY + row * a.dy_ld + col, a.cols - col, d[c]);
+      load8(Z + row * a.z_ld + col, a.cols - col, zh[c]);
+    }
+    const float rstd = a.rstd[row];
+    float s = 0.0f;
+#pragma unroll
+    for (int c = 0; c < NCH; ++c)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        zh[c][i] *= rstd;
+        dg[c][i] = fmaf(d[c][i], zh[c][i], dg[c][i]);
+        d[c][i] *= g[c][i];
+        s = fmaf(d[c][i], zh[c][i], s);
+      }
+    if (DX == nullptr) continue;
+    const float m = row_sum<TPR>(s, red) * inv;
+#pragma unroll
+    for (int c = 0; c < NCH; ++c) {
+      const int col = 8 * (t + TPR * c);
+      float r[8] = {};
+      if (DZ != nullptr) load8(DZ + row * a.dz_ld + col, a.cols - col, r);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) r[i] = fmaf(rstd, fmaf(-zh[c][i], m, d[c][i]), r[i]);
+      store8(DX + row * a.dx_ld + col, a.cols - col, r);
+    }
+  }
+  if (a.part == nullptr) return;
+  if constexpr (kPer > 1) {
+#pragma unroll 1
+    for (int w = kPer - 1; w >= 0; --w) {       // the last wave first, wave 0 keeps the sum
+      if ((int)(threadIdx.x / TPR) == w) {
+#pragma unroll
+        for (int c = 0; c < NCH; ++c)
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            float& slot = joint[(c * 8 + i) * TPR + t];
+            if (w < kPer - 1) dg[c][i] += slot;
+            slot = dg[c][i];
+          }
+      }
+      __syncthreads();
+    }
+    if (threadIdx.x >= TPR) return;
+  }
+#pragma unroll
+  for (int c = 0; c < NCH; ++c) {
+    const int col = 8 * (t + TPR * c);
+    store8(a.part + (int64_t)blockIdx.x * a.cols + col, a.cols - col, dg[c]);
+  }
+}
+
+// Rows longer than a workgroup's registers: two passes over the row, the share
+// of dgain in the workgroup's own row of `part`.
+template <typename T>
+__global__ __launch_bounds__(1024) void rms_bwd_long_kernel(RmsBwd a) {
+  __shared__ float red[16];
+  const T* DY = (const T*)a.dy;
+  const T* Z = (const T*)a.z;
+  const T* DZ = (const T*)a.dz;
+  T* DX = (T*)a.dx;
+  float* part = a.part == nullptr ? nullptr : a.part + (int64_t)blockIdx.x * a.cols;
+  bool first = true;
+  for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
+    const float rstd = a.rstd[row];
+    float s = 0.0f;
+    for (int col = 8 * threadIdx.x; col < a.cols; col += 8192) {
+      float d[8], z[8], w[8] = {};
+      load8(DY + row * a.dy_ld + col, a.cols - col, d);
+      load8(Z + row * a.z_ld + col, a.cols - col, z);
+      if (part != nullptr) {
+        if (!first) load8(part + col, a.cols - col, w);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) w[i] = fmaf(d[i], z[i] * rstd, w[i]);
+        store8(part + col, a.cols - col, w);
+      }
+#pragma unroll
+      for (int i = 0; i < 8; ++i) w[i] = 1.0f;
+      if (a.gain != nullptr) load8(a.gain + col, a.cols - col, w);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) s = fmaf(d[i] * w[i], z[i] * rstd, s);
+    }
+    first = false;
+    if (DX == nullptr) continue;
+    const float m = row_sum<1024>(s, red) / (float)a.cols;
+    for (int col = 8 * threadIdx.x; col < a.cols; col += 8192) {
+      float d[8], z[8], w[8], r[8] = {};
+      load8(DY + row * a.dy_ld + col, a.cols - col, d);
+      load8(Z + row * a.z_ld + col, a.cols - col, z);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) w[i] = 1.0f;
+      if (a.gain != nullptr) load8(a.gain + col, a.cols - col, w);
+      if (DZ != nullptr) load8(DZ + row * a.dz_ld + col, a.cols - col, r);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) r[i] = fmaf(rstd, fmaf(-(z[i] * rstd), m, d[i] * w[i]), r[i]);
+      store8(DX + row * a.dx_ld + col, a.cols - col, r);
+    }
+  }
+}
+
+// out[c] = sum over the n rows of part, in a fixed order: a workgroup takes 32
+// columns, 32 threads a column with the rows r, r + 32, ...; their sums are
+// added in order.
+__global__ __launch_bounds__(1024) void part_sum_kernel(const float* __restrict__ part, float* __restrict__ out, int n,
+                                                       int cols) {
+  __shared__ float s[32][33];
+  const int c = threadIdx.x & 31, r = threadIdx.x >> 5;
+  const int col = blockIdx.x * 32 + c;
+  float x[4] = {};
+  if (col < cols) {
+    int k = r;
+    for (; k + 96 < n; k += 128)
+#pragma unroll
+      for (int u = 0; u < 4; ++u) x[u] += part[(int64_t)(k + 32 * u) * cols + col];
+    for (; k < n; k += 32) x[0] += part[(int64_t)k * cols + col];
+  }
+  s[r][c] = (x[0] + x[1]) + (x[2] + x[3]);
+  __syncthreads();
+  if (r == 0 && col < cols) {
+    float sum = 0.0f;
+#pragma unroll
+    for (int k = 0; k < 32; ++k) sum += s[k][c];
+    out[col] = sum;
+  }
+}
+
+// Threads a row and chunks a thread.  One wave a row up to 2048 columns, where
+// rows are many: a row's sums then need no barrier.  Few rows, and longer
+// ones, take a workgroup each.
+struct RowForm {
+  int tpr, nch;           // tpr 0: the long form
+};
+RowForm row_form(int64_t rows, int cols) {
+  const int chunks = (cols + 7) / 8;
+  auto pick = [&](int tpr) { return RowForm{tpr, chunks <= tpr ? 1 : chunks <= 2 * tpr ? 2 : 4}; };
+  if (chunks <= 64 || (chunks <= 256 && rows > 1024)) return pick(64);
+  if (chunks <= 512 || (chunks <= 1024 && rows > 256)) return pick(256);
+  if (chunks <= 4096) return pick(1024);
+  return RowForm{0, 0};
+}
+
+}  // namespace
+
+#define TERRA_ROW_FORMS(KERNEL, T)                                                                   \
+  switch (f.tpr + f.nch) {                                                                           \
+    case 65: hipLaunchKernelGGL((KERNEL<T, 64, 1>), grid, dim3(256), 0, st, a); break;               \
+    case 66: hipLaunchKernelGGL((KERNEL<T, 64, 2>), grid, dim3(256), 0, st, a); break;               \
+    case 68: hipLaunchKernelGGL((KERNEL<T, 64, 4>), grid, dim3(256), 0, st, a); break;               \
+    case 257: hipLaunchKernelGGL((KERNEL<T, 256, 1>), grid, dim3(256), 0, st, a); break;             \
+    case 258: hipLaunchKernelGGL((KERNEL<T, 256, 2>), grid, dim3(256), 0, st, a); break;             \
+    case 260: hipLaunchKernelGGL((KERNEL<T, 256, 4>), grid, dim3(256), 0, st, a); break;             \
+    case 1025: hipLaunchKernelGGL((KERNEL<T, 1024, 1>), grid, dim3(1024), 0, st, a); break;          \
+    case 1026: hipLaunchKernelGGL((KERNEL<T, 1024, 2>), grid, dim3(1024), 0, st, a); break;          \
+    case 1028: hipLaunchKernelGGL((KERNEL<T, 1024, 4>), grid, dim3(1024), 0, st, a); break;          \
+  }
+
+namespace {
+
+int row_blocks(int64_t rows, int per, int most) {
+  const int64_t b = (rows + per - 1) / per;
+  return (int)(b < most ? b : most);
+}
+
+template <typename T>
+hipError_t fwd_t(const RmsFwd& a, hipStream_t st) {
+  const RowForm f = row_form(a.rows, a.cols);
+  // enough workgroups for eight waves a SIMD on 256 compute units
+  const dim3 grid(row_blocks(a.rows, f.tpr == 64 ? 4 : 1, f.tpr == 1024 || f.tpr == 0 ? 512 : 2048));
+  if (f.tpr == 0) hipLaunchKernelGGL(rms_fwd_long_kernel<T>, grid, dim3(1024), 0, st, a);
+  TERRA_ROW_FORMS(rms_fwd_kernel, T)
+  return hipGetLastError();
+}
+
+template <typename T>
+hipError_t bwd_t(const RmsBwd& a, int blocks, hipStream_t st) {
+  const RowForm f = row_form(a.rows, a.cols);
+  const dim3 grid(blocks);
+  if (f.tpr == 0) hipLaunchKernelGGL(rms_bwd_long_kernel<T>, grid, dim3(1024), 0, st, a);
+  TERRA_ROW_FORMS(rms_bwd_kernel, T)
+  return hipGetLastError();
+}
+
+}  // namespace
+#undef TERRA_ROW_FORMS
+
+hipError_t launch_part_sum(const float* part, float* out, int n, int cols, hipStream_t st) {
+  hipLaunchKernelGGL(part_sum_kernel, dim3((cols + 31) / 32), dim3(1024), 0, st, part, out, n, cols);
+  return hipGetLastError();
+}
+
+// Workgroups of the backward, each with a row of partial sums.
+int rms_bwd_blocks(int64_t rows, int cols) {
+  const RowForm f = row_form(rows, cols);
+  return row_blocks(rows, f.tpr == 64 ? 4 : 1, f.tpr == 1024 || f.tpr == 0 ? 512 : 1024);
+}
+
+hipError_t launch_rms_fwd(int dtype, const RmsFwd& a, hipStream_t st) {
+  if (a.rows == 0) return hipSuccess;
+  return dtype == 0 ? fwd_t<float>(a, st) : dtype == 1 ? fwd_t<__bf16>(a, st) : fwd_t<_Float16>(a, st);
+}
+
+hipError_t launch_rms_bwd(int dtype, const RmsBwd& a, float* dgain, hipStream_t st) {
+  const int blocks = rms_bwd_blocks(a.rows, a.cols);
+  if (blocks > 0 && (a.dx != nullptr || dgain != nullptr)) {
+    const hipError_t e = dtype == 0   ? bwd_t<float>(a, blocks, st)
+                         : dtype == 1 ? bwd_t<__bf16>(a, blocks, st)
+                                      : bwd_t<_Float16>(a, blocks, st);
+    if (e != hipSuccess) return e;
+  }
+  return dgain == nullptr ? hipSuccess : launch_part_sum(a.part, dgain, blocks, a.cols, st);
+}
+
+}  // namespace terra

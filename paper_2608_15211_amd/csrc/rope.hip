@@ -1,0 +1,190 @@
+// rope.hip - rotary positions: pairs of a head's channels turned by the angle
+// of the token's position, on q and k in one launch.
+//
+//   (a, b) -> scale (a cos - b sin, a sin + b cos),  angle = position * f_i
+// Pair i of an axis holds channels (2i, 2i + 1) of its part of the head, or
+// (i, i + half).  The backward is the same with the angles' signs turned.
+//
+// Angles.  position * f_i loses every digit that counts in float32 at far
+// positions, so a frequency comes as turns a position in 64-bit fixed point
+// and the product is taken modulo 2^64, which drops the whole turns exactly:
+// an angle is off by at most |position| * 2^-65 turns besides the float32
+// steps after it, at any 32-bit position.
+//
+// What bounds it: HBM, every channel is read and written once.  A workgroup
+// takes `tb` tokens: it first works out their cosines and sines, once for all
+// heads of q and k, into LDS, then moves units of V pairs, consecutive threads
+// along a head.
+#include <math.h>
+
+#include <algorithm>
+
+#include "terra_vec.h"
+#include "terra_ops.h"
+
+namespace terra {
+
+namespace {
+
+// cos and sin of u / 2^32 turns: the quadrant from the two leading bits (after
+// rounding), the rest, |x| <= pi / 4, by the Taylor polynomials to x^9 and x^8
+// (next terms below 2e-9 and 3e-8).
+__device__ inline float2 cos_sin(uint32_t u) {
+  const uint32_t quad = (u + 0x20000000u) >> 30;
+  const float x = (float)(int32_t)(u - (quad << 30)) * 1.46291807926715968e-9f;   // 2 pi / 2^32
+  const float y = x * x;
+  const float s = fmaf(x * y, fmaf(y, fmaf(y, fmaf(y, 2.7557319e-6f, -1.9841270e-4f), 8.3333333e-3f), -1.6666667e-1f), x);
+  const float c = fmaf(y, fmaf(y, fmaf(y, fmaf(y, 2.4801587e-5f, -1.3888889e-3f), 4.1666667e-2f), -0.5f), 1.0f);
+  const bool swap = quad & 1;
+  const float cs = swap ? s : c, sn = swap ? c : s;
+  return float2{((quad + 1) & 2) ? -cs : cs, (quad & 2) ? -sn : sn};
+}
+
+template <typename T, int V>
+struct Vec {
+  T v[V];
+};
+
+// Threads a workgroup, and the LDS floats its angles may take.
+constexpr int kRopeThreads = 256;
+constexpr int kRopeAngles = 4096;
+
+template <typename T, int V, bool HALF>
+__global__ __launch_bounds__(kRopeThreads) void rope_kernel(RopeArgs a) {
+  extern __shared__ float2 angles[];       // [tb][pairs]
+  const int64_t blocks = (a.tokens + a.tb - 1) / a.tb;
+  for (int64_t blk = blockIdx.x; blk < blocks; blk += gridDim.x) {
+    if (blk != blockIdx.x) __syncthreads();     // the angles of the last tokens are used
+    const int64_t tok0 = blk * a.tb;
+    const int ntok = (int)min((int64_t)a.tb, a.tokens - tok0);
+    for (int idx = threadIdx.x; idx < ntok * a.pairs; idx += kRopeThreads) {
+      const int t = fast_div(idx, a.pairs, a.rpairs), p = idx - t * a.pairs;
+      const int axis = p >= a.half ? 1 : 0;
+      const int64_t tok = tok0 + t;
+      int64_t pos;
+      if (a.pos != nullptr) {
+        pos = a.pos[tok * a.axes + axis];
+      } else {
+        const uint32_t cell = (uint32_t)(tok % (int64_t)a.grid_hw);
+        pos = a.axes == 1 ? cell : axis == 0 ? cell / (uint32_t)a.grid_w : cell % (uint32_t)a.grid_w;
+      }
+      float2 cs = cos_sin((uint32_t)(((uint64_t)pos * a.turns[p - axis * a.half]) >> 32));
+      angles[idx] = float2{cs.x * a.scale, cs.y * a.sin_scale};
+    }
+    __syncthreads();
+
+    // units of a token: q's heads, then k's; a head's turned units of V pairs,
+    // then the copied ones of 2 V channels
+    const int total = ntok * a.units;
+    for (int idx = threadIdx.x; idx < total; idx += kRopeThreads) {
+      const int t = fast_div(idx, a.units, a.runits);
+      const int rem = idx - t * a.units;
+      int head = fast_div(rem, a.uph, a.ruph);
+      const int u = rem - head * a.uph;
+      const bool second = head >= a.side[0].heads;
+      const RopeSide& s = second ? a.side[1] : a.side[0];
+      if (second) head -= a.side[0].heads;
+      const T* in = (const T*)s.in + (tok0 + t) * s.in_t + head * s.in_h;
+      T* out = (T*)s.out + (tok0 + t) * s.out_t + head * s.out_h;
+      if (u < a.turned) {
+        const int p = u * V;
+        const float2* cs = angles + t * a.pairs + p;
+        if (HALF) {
+          const int lo = p + (p >= a.half ? a.half : 0);     // channel of the first of each pair
+          Vec<T, V> x, y;
+          __builtin_memcpy(&x, in + lo, sizeof(x));
+          __builtin_memcpy(&y, in + lo + a.half, sizeof(y));
+  #pragma unroll
+          for (int i = 0; i < V; ++i) {
+            const float2 c = cs[i];
+            const float xf = to_float<T>(x.v[i]), yf = to_float<T>(y.v[i]);
+            x.v[i] = from_float<T>(fmaf(xf, c.x, -yf * c.y));
+            y.v[i] = from_float<T>(fmaf(xf, c.y, yf * c.x));
+          }
+          __builtin_memcpy(out + lo, &x, sizeof(x));
+          __builtin_memcpy(out + lo + a.half, &y, sizeof(y));
+        } else {
+          Vec<T, 2 * V> x;
+          __builtin_memcpy(&x, in + 2 * p, sizeof(x));
+  #pragma unroll
+          for (int i = 0; i < V; ++i) {
+            const float2 c = cs[i];
+            const float xf = to_float<T>(x.v[2 * i]), yf = to_float<T>(x.v[2 * i + 1]);
+            x.v[2 * i] = from_float<T>(fmaf(xf, c.x, -yf * c.y));
+            x.v[2 * i + 1] = from_float<T>(fmaf(xf, c.y, yf * c.x));
+          }
+          __builtin_memcpy(out + 2 * p, &x, sizeof(x));
+        }
+      } else {
+        const int c0 = 2 * a.pairs + (u - a.turned) * 2 * V;
+        if (c0 + 2 * V <= a.hd) {
+          Vec<T, 2 * V> x;
+          __builtin_memcpy(&x, in + c0, sizeof(x));
+          __builtin_memcpy(out + c0, &x, sizeof(x));
+        } else {
+          for (int c = c0; c < a.hd; ++c) out[c] = in[c];
+        }
+      }
+    }
+  }
+}
+
+template <typename T, int V>
+hipError_t rope_form(const RopeArgs& a, bool half, hipStream_t st) {
+  const dim3 grid((unsigned)std::min<int64_t>((a.tokens + a.tb - 1) / a.tb, 1 << 20));
+  const size_t lds = (size_t)a.tb * a.pairs * sizeof(float2);
+  if (half) hipLaunchKernelGGL((rope_kernel<T, V, true>), grid, dim3(kRopeThreads), lds, st, a);
+  else hipLaunchKernelGGL((rope_kernel<T, V, false>), grid, dim3(kRopeThreads), lds, st, a);
+  return hipGetLastError();
+}
+
+template <typename T>
+hipError_t rope_t(const RopeArgs& a, int v, bool half, hipStream_t st) {
+  return v == 8   ? rope_form<T, 8>(a, half, st)
+         : v == 4 ? rope_form<T, 4>(a, half, st)
+         : v == 2 ? rope_form<T, 2>(a, half, st)
+                  : rope_form<T, 1>(a, half, st);
+}
+
+}  // namespace
+
+// turns[i] = f_i / (2 pi) in units of 2^-64, for the pairs of one axis.
+void rope_turns(double base, int scaling, double factor, double orig_len, double beta_fast, double beta_slow, int part,
+                uint64_t* turns) {
+  const long double two_pi = 6.283185307179586476925286766559005768L;
+  if (scaling == 2) base *= pow(factor, (double)part / (part - 2));
+  for (int i = 0; i < part / 2; ++i) {
+    long double f = powl((long double)base, -2.0L * i / part) / two_pi;
+    if (scaling == 1) f /= factor;
+    if (scaling == 3) {
+      long double keep = (orig_len * f - beta_slow) / (beta_fast - beta_slow);
+      keep = keep < 0 ? 0 : keep > 1 ? 1 : keep;
+      f *= keep + (1 - keep) / factor;
+    }
+    turns[i] = (uint64_t)ldexpl(f, 64);
+  }
+}
+
+hipError_t launch_rope(int dtype, RopeArgs a, bool half, hipStream_t st) {
+  if (a.tokens == 0) return hipSuccess;
+  // the most pairs a unit: 8 (16-byte accesses of 16-bit types), fewer where
+  // they do not divide an axis's pairs
+  int v = 8;
+  while (a.half % v != 0) v /= 2;
+  const bool copy = a.hd > 2 * a.pairs && !(a.side[0].in == a.side[0].out && (a.side[1].heads == 0 || a.side[1].in == a.side[1].out));
+  a.turned = a.pairs / v;
+  a.uph = a.turned + (copy ? (a.hd - 2 * a.pairs + 2 * v - 1) / (2 * v) : 0);
+  a.units = a.uph * (a.side[0].heads + a.side[1].heads);
+  // tokens a workgroup: about six units a thread, while the angles fit, and
+  // fewer where that would leave compute units idle
+  int64_t tb = (6 * kRopeThreads + a.units - 1) / a.units;
+  tb = std::min<int64_t>(tb, std::max(1, kRopeAngles / a.pairs));
+  tb = std::min<int64_t>(tb, std::max<int64_t>(1, a.tokens / 512));
+  a.tb = (int)tb;
+  a.rpairs = 1.0f / (float)a.pairs;
+  a.runits = 1.0f / (float)a.units;
+  a.ruph = 1.0f / (float)a.uph;
+  return dtype == 0 ? rope_t<float>(a, v, half, st) : dtype == 1 ? rope_t<__bf16>(a, v, half, st) : rope_t<_Float16>(a, v, half, st);
+}
+
+}  // namespace terra
