@@ -40,7 +40,8 @@ __device__ inline i32x8 join(const bf16x8& lo, const bf16x8& hi) {
 }
 
 // One half of a stage (32 contraction indices, of 8-bit elements 64): a
-// wave's MI x 2 blocks of 32 x 32.
+// wave's MI x 2 blocks of 32 x 32.  B is the instruction's first operand, so
+// that a lane's sixteen results are columns of one row of the output.
 template <typename T, int MI>
 __device__ __forceinline__ void stage_products(f32x16 (&acc)[MI][2], const bf16x8 (&ao)[2][MI],
                                                const bf16x8 (&bo)[2][2]) {
@@ -49,7 +50,7 @@ __device__ __forceinline__ void stage_products(f32x16 (&acc)[MI][2], const bf16x
     for (int i = 0; i < MI; ++i)
 #pragma unroll
       for (int j = 0; j < 2; ++j)
-        acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(join(ao[0][i], ao[1][i]), join(bo[0][j], bo[1][j]),
+        acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(join(bo[0][j], bo[1][j]), join(ao[0][i], ao[1][i]),
                                                                     acc[i][j], 0, 0, 0, kUnitScale, 0, kUnitScale);
   } else {
 #pragma unroll
@@ -58,121 +59,11 @@ __device__ __forceinline__ void stage_products(f32x16 (&acc)[MI][2], const bf16x
       for (int i = 0; i < MI; ++i)
 #pragma unroll
         for (int j = 0; j < 2; ++j)
-          mma16(acc[i][j], __builtin_bit_cast(typename Operand<T>::type, ao[c][i]),
-                __builtin_bit_cast(typename Operand<T>::type, bo[c][j]));
+          mma16(acc[i][j], __builtin_bit_cast(typename Operand<T>::type, bo[c][j]),
+                __builtin_bit_cast(typename Operand<T>::type, ao[c][i]));
   }
 }
 
-// The products of a workgroup tile's `nk` stages into acc.  issue_a(s, st)
-// starts the loads of stage s of A into buffer st of its ring, issue_b those
-// of B; every thread calls both.  Eight waves: the two waves of a SIMD take
-// turns at LDS and the matrix cores; four waves: three stages in flight.
-// (The Swin block's kernel holds the same two schedules and what they were
-// measured against.)
-template <typename T, bool KROW, int NW, class IssueA, class IssueB>
-__device__ __forceinline__ void gemm_stages(bf16* lds, int nk, f32x16 (&acc)[NW == 8 ? 4 : 2][2],
-                                            const IssueA& issue_a, const IssueB& issue_b) {
-  constexpr int NT = NW * 64, BM = NW == 8 ? kBM : kBS, BN = BM, BK = kBK, MI = BM / 64;
-  const int lane = threadIdx.x & 63;
-  const int wave = threadIdx.x >> 6;
-  const int wm = (wave / (NW / 2)) * 32 * MI, wn = (wave % (NW / 2)) * 64;
-  typedef Tile<BM, KROW, BK, NT> TA;
-  typedef Tile<BN, KROW, BK, NT> TB;
-  // LDS rings: kRA stages of A, then two (four waves: four) of B
-  constexpr int kRA = NW == 8 ? 3 : 4;
-  auto a_tile = [&](int st) { return lds + st * TA::kElems; };
-  auto b_tile = [&](int st) { return lds + kRA * TA::kElems + st * TB::kElems; };
-  bf16x8 ao[2][MI], bo[2][2];
-  // operands of the 32 contraction indices from 32 * hf of a stage
-  auto read_ops = [&](const bf16* ta, const bf16* tb, int hf) {
-#pragma unroll
-    for (int c = 0; c < 2; ++c) {
-      const int k0 = 32 * hf + 16 * c;
-#pragma unroll
-      for (int j = 0; j < 2; ++j)
-        bo[c][j] = KROW ? row_operand<BN, BK>(tb, k0, wn + 32 * j, lane) : tr_operand<BN, BK>(tb, k0, wn + 32 * j, lane);
-#pragma unroll
-      for (int i = 0; i < MI; ++i)
-        ao[c][i] =
-            KROW ? row_operand<BM, BK>(ta, k0, wm + 32 * i, lane) : tr_operand<BM, BK>(ta, k0, wm + 32 * i, lane);
-    }
-  };
-  auto mfmas = [&]() { stage_products<T>(acc, ao, bo); };
-  if constexpr (NW == 8) {
-    // Turn 4 kt + 2 hf: the first half of the workgroup reads half hf of
-    // stage kt, the second half multiplies what it read in its last turn;
-    // in the next turn they swap.  A stage's buffer is free after turn
-    // 4 kt + 3, so the loads of B's stage kt + 1 (two buffers) go out while
-    // half 0 of stage kt is read, those of A's stage kt + 2 (three) while
-    // half 1 is.
-    const bool second = __builtin_amdgcn_readfirstlane(wave) >= NW / 2;
-    if (nk > 0) {
-      issue_a(0, 0);
-      issue_b(0, 0);
-    }
-    if (nk > 1) {
-      issue_a(1, 1);
-      wait_vm<TA::kPer>();
-    } else {
-      wait_vm<0>();
-    }
-    lds_barrier();
-    if (second) lds_barrier();
-    int sa3 = 0;               // kt % 3
-    for (int kt = 0; kt < nk; ++kt) {
-      const bf16* ta = a_tile(sa3);
-      const bf16* tb = b_tile(kt & 1);
-#pragma unroll
-      for (int hf = 0; hf < 2; ++hf) {
-        read_ops(ta, tb, hf);
-        if (hf == 0) {
-          if (kt + 1 < nk) issue_b(kt + 1, (kt + 1) & 1);
-        } else {
-          if (kt + 2 < nk) issue_a(kt + 2, sa3 == 0 ? 2 : sa3 - 1);
-        }
-        auto wait_next = [&]() {     // stage kt + 1 is in LDS (A of stage kt + 2 may be in flight)
-          if (hf == 1) {
-            if (kt + 2 < nk) wait_vm<TA::kPer>();
-            else wait_vm<0>();
-          }
-        };
-        if (second) wait_next();
-        __builtin_amdgcn_sched_barrier(0);
-        lds_barrier();
-        __builtin_amdgcn_sched_barrier(0);
-        __builtin_amdgcn_s_setprio(1);
-        mfmas();
-        __builtin_amdgcn_s_setprio(0);
-        __builtin_amdgcn_sched_barrier(0);
-        if (!second) wait_next();
-        lds_barrier();
-        __builtin_amdgcn_sched_barrier(0);
-      }
-      sa3 = sa3 == 2 ? 0 : sa3 + 1;
-    }
-    if (!second) lds_barrier();
-  } else {
-    constexpr int kLoads = TA::kPer + TB::kPer;
-    for (int s = 0; s < 3; ++s)
-      if (s < nk) { issue_a(s, s); issue_b(s, s); }
-    for (int kt = 0; kt < nk; ++kt) {
-      const int left = nk - 1 - kt;      // stages after this one
-      if (left >= 2) wait_vm<2 * kLoads>();
-      else if (left == 1) wait_vm<kLoads>();
-      else wait_vm<0>();
-      lds_barrier();     // stage kt is in LDS, and every wave is done with the one before
-      if (left >= 3) {
-        issue_a(kt + 3, (kt + 3) & 3);
-        issue_b(kt + 3, (kt + 3) & 3);
-      }
-#pragma unroll
-      for (int hf = 0; hf < 2; ++hf) {
-        read_ops(a_tile(kt & 3), b_tile(kt & 3), hf);
-        mfmas();
-      }
-    }
-  }
-}
 
 // ---------------------------------------------------------------------------
 // Operands of any alignment and length: 16-byte chunks pass through registers
@@ -262,21 +153,25 @@ struct LinEpi {
 // Constants of eight columns.
 struct LinCols {
   float bias[8], scale[8];
-  __device__ LinCols(const LinEpi& e, int n, int nv) {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) { bias[i] = 0.0f; scale[i] = 1.0f; }
-    if (e.bias != nullptr) load8(e.bias + n, nv, bias);
-    if (e.w_scale != nullptr) load8(e.w_scale + n, nv, scale);
-  }
 };
+__device__ inline LinCols lin_cols(const LinEpi& e, int n, int nv) {
+  LinCols c;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) { c.bias[i] = 0.0f; c.scale[i] = 1.0f; }
+  if (e.bias != nullptr) load8(e.bias + n, nv, c.bias);
+  if (e.w_scale != nullptr) load8(e.w_scale + n, nv, c.scale);
+  return c;
+}
 
 // Columns [n, n + 8) (nv of them inside) of row m.
 template <typename TO>
-__device__ inline void finish8(const LinEpi& e, const LinCols& c, int64_t m, int n, int nv, float (&v)[8]) {
+__device__ __forceinline__ void finish_row8(const LinEpi& e, const LinCols& c, int64_t m, int n, int nv, float (&v)[8]) {
+  float res[8];
+  if (e.res != nullptr) load8((const TO*)e.res + m * e.res_ld + n, nv, res);
   if (e.x_scale != nullptr) {
-    const float s = e.x_scale[m];
+    const float xs = e.x_scale[m];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = fmaf(v[i] * s, c.scale[i], c.bias[i]);
+    for (int i = 0; i < 8; ++i) v[i] = fmaf(v[i] * xs, c.scale[i], c.bias[i]);
   } else {
 #pragma unroll
     for (int i = 0; i < 8; ++i) v[i] += c.bias[i];
@@ -284,12 +179,64 @@ __device__ inline void finish8(const LinEpi& e, const LinCols& c, int64_t m, int
   if (e.pre != nullptr) store8((TO*)e.pre + m * e.pre_ld + n, nv, v);
   activate(v, e.act);
   if (e.res != nullptr) {
-    float r[8];
-    load8((const TO*)e.res + m * e.res_ld + n, nv, r);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] += r[i];
+    for (int i = 0; i < 8; ++i) v[i] += res[i];
   }
   store8((TO*)e.y + m * e.y_ld + n, nv, v);
+}
+
+// A wave's results on their way out: ROWS x 64 float32 in its part of LDS, 16-byte
+// chunk c of row m at chunk c ^ (m % 16) (writes of a lane's own rows and reads of
+// whole rows then hit every bank once).  A lane takes 8 columns of rows 8 t + lane / 8,
+// so that eight lanes store a row's 128 bytes (stores of 32 bytes a row straight
+// from the registers: 138240 x 2304 x 768 in 681 us against 547).  One copy of
+// the loop for every block of a tile: unrolled over them the code no longer fits
+// the instruction cache (an epilogue of 22 us a tile).
+template <typename TO, bool F32, int ROWS>
+__device__ __forceinline__ void drain(const LinEpi& e, const float* et, float col_bias, float col_scale, int64_t m0, int64_t M, int n0,
+                                      int N, int z) {
+  const int lane = threadIdx.x & 63, er = lane >> 3, ec = lane & 7;
+  const int n = n0 + 8 * ec, nv = N - n;
+  LinCols lc;
+  if constexpr (!F32) {
+#pragma unroll
+    for (int x = 0; x < 8; ++x) lc.bias[x] = __shfl(col_bias, 8 * ec + x, 64);
+    if (e.x_scale != nullptr) {
+#pragma unroll
+      for (int x = 0; x < 8; ++x) lc.scale[x] = __shfl(col_scale, 8 * ec + x, 64);
+    }
+  }
+  auto rows = [&](auto whole_c) {
+    constexpr bool kWhole = decltype(whole_c)::value;
+    const int left = kWhole ? 8 : nv;
+#pragma unroll 4
+    for (int t = 0; t < ROWS / 8; ++t) {
+      const int row = 8 * t + er;
+      const int64_t m = m0 + row;
+      const f32x4 lo = *reinterpret_cast<const f32x4*>(et + row * 64 + 4 * ((2 * ec) ^ (row & 15)));
+      const f32x4 hi = *reinterpret_cast<const f32x4*>(et + row * 64 + 4 * ((2 * ec + 1) ^ (row & 15)));
+      float v[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+      if (!kWhole && (m >= M || nv <= 0)) continue;
+      if constexpr (F32) {
+        store8(e.outf + z * e.f_slice + m * e.f_ld + n, left, v);
+      } else {
+        finish_row8<TO>(e, lc, m, n, left, v);
+      }
+    }
+  };
+  if (m0 + ROWS <= M && n0 + 64 <= N) rows(std::true_type{});
+  else rows(std::false_type{});
+}
+
+// Tile w of an nM x nN grid of tiles, above 12 columns in panels of up to eight, rows in turn within one:
+// the 32 tiles that an XCD's compute units work on at a time are then about 4 x 8
+// and share most of what they read.
+__device__ inline void panel_place(int w, int nM, int nN, int& tm, int& tn) {
+  const int panels = nN <= 12 ? 1 : (nN + 7) >> 3, width = (nN + panels - 1) / panels;
+  const int p = w / (nM * width), c = min(width, nN - p * width);
+  w -= p * nM * width;
+  tm = w / c;
+  tn = p * width + w - tm * c;
 }
 
 struct GemmArgs {
@@ -299,129 +246,304 @@ struct GemmArgs {
   int N, K;                // K in 16-bit units
   int kslice;              // units of a contraction slice, whole stages
   int row_bytes;           // KROW: bytes of a row
+  int work;                // (slice, tile) pairs
   LinEpi e;
 };
 
-// out[M][N] = sum over k of A(m, k) B(n, k).  The grid holds (slice, tile)
-// pairs; NW 8, 4, or 0: four waves with operands through registers.
-// F32: float32 sums of the slice, else the epilogue.
+// Pure instructions may be moved across barriers and priorities: these keep the
+// matrix instructions between them.
+template <int MI>
+__device__ __forceinline__ void pin(bf16x8 (&o)[2][MI]) {
+#pragma unroll
+  for (int c = 0; c < 2; ++c)
+#pragma unroll
+    for (int i = 0; i < MI; ++i) asm volatile("" : "+v"(o[c][i]));
+}
+template <int MI>
+__device__ __forceinline__ void pin_sums(f32x16 (&acc)[MI][2]) {
+#pragma unroll
+  for (int i = 0; i < MI; ++i)
+#pragma unroll
+    for (int j = 0; j < 2; ++j) asm volatile("" : "+v"(acc[i][j]));
+}
+
+// out[M][N] = sum over k of A(m, k) B(n, k).  NW 8, 4, or 0: four waves with
+// operands through registers.  F32: float32 sums of the slice, else the
+// epilogue.
+//
+// Work.  There are `work` (slice, tile) pairs; each XCD takes one contiguous run of
+// them, so that tiles sharing operand rows share an L2, and its workgroups take
+// the run's pairs in turn.  The loads of a workgroup's next tile go out before
+// the epilogue of the last: the matrix cores do not wait for a cold start at
+// each tile.
+// Stages.  The two waves of a SIMD (w and w + 4) take turns: one half of the
+// workgroup multiplies while the other reads its next operands from LDS and
+// issues loads, with a barrier after each turn (eight waves); four waves keep
+// three stages in flight.
 template <typename T, typename TO, bool KROW, int NW, bool F32>
 __global__ __launch_bounds__(NW == 8 ? 512 : 256, 1) void lin_gemm_kernel(GemmArgs g) {
   constexpr int W = NW == 8 ? 8 : 4, NT = W * 64, BM = NW == 8 ? kBM : kBS, BN = BM;
   constexpr int MI = BM / 64, kWM = 32 * MI;
   extern __shared__ __align__(16) char smem[];
   bf16* lds = reinterpret_cast<bf16*>(smem);
+  typedef Tile<BM, KROW, kBK, NT> TL;
+  constexpr int kRA = NW == 8 ? 3 : 4;         // stages of A's ring; B's is two (four waves: four)
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wm = (wave / (W / 2)) * kWM, wn = (wave % (W / 2)) * 64;
   const int nN = (g.N + BN - 1) / BN;
-  const int tiles = (int)((g.M + BM - 1) / BM) * nN;
-  // Workgroups go to the 8 XCDs in turn; each XCD takes one contiguous run of
-  // (slice, tile) pairs, so that tiles sharing operand rows share an L2.
-  const int total = gridDim.x, xcd = blockIdx.x & 7;
-  const int w0 = xcd * (total >> 3) + min(xcd, total & 7) + (blockIdx.x >> 3);
-  const int z = w0 / tiles, w = w0 - z * tiles;
-  const int tm = w / nN, tn = w - tm * nN;
-  const int64_t m0 = (int64_t)tm * BM;
-  const int n0 = tn * BN;
-  const int kbeg = z * g.kslice, klen = min(g.K - kbeg, g.kslice);
-  const int nk = (klen + kBK - 1) / kBK;
-  const int rows = (int)min((int64_t)BM, g.M - m0), cols = min(BN, g.N - n0);
-  // the tile's operands at the slice's first contraction index
-  const char* pa = g.a + (KROW ? m0 * g.lda + 2 * (int64_t)kbeg : kbeg * g.lda + 2 * m0);
-  const char* pb = g.b + (KROW ? n0 * g.ldb + 2 * (int64_t)kbeg : kbeg * g.ldb + 2 * (int64_t)n0);
+  const int nM = (int)((g.M + BM - 1) / BM), tiles = nM * nN;
+  const int xcd = blockIdx.x & 7;
+  const int peers = ((int)gridDim.x - xcd + 7) >> 3;               // workgroups of this XCD
+  int w0 = xcd * (g.work >> 3) + min(xcd, g.work & 7);
+  const int wend = w0 + (g.work >> 3) + (xcd < (g.work & 7) ? 1 : 0);
+  w0 += blockIdx.x >> 3;
+
+  // the tile that is being multiplied, and the one whose loads are going out
+  struct Place {
+    int64_t m0;
+    int n0, z, klen, nk;
+  };
+  auto place = [&](int w) {
+    Place p;
+    p.z = w / tiles;
+    w -= p.z * tiles;
+    int tm, tn;
+    panel_place(w, nM, nN, tm, tn);
+    p.m0 = (int64_t)tm * BM;
+    p.n0 = tn * BN;
+    p.klen = min(g.K - p.z * g.kslice, g.kslice);
+    p.nk = (p.klen + kBK - 1) / kBK;
+    return p;
+  };
   f32x16 acc[MI][2];
+  auto clear = [&]() {
 #pragma unroll
-  for (int i = 0; i < MI; ++i)
+    for (int i = 0; i < MI; ++i)
 #pragma unroll
-    for (int j = 0; j < 2; ++j) acc[i][j] = f32x16{};
+      for (int j = 0; j < 2; ++j) acc[i][j] = f32x16{};
+  };
+  bf16x8 ao[2][MI], bo[2][2];
+  auto read_ops = [&](const bf16* ta, const bf16* tb, int hf) {
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+      const int k0 = 32 * hf + 16 * c;
+#pragma unroll
+      for (int j = 0; j < 2; ++j)
+        bo[c][j] = KROW ? row_operand<BN, kBK>(tb, k0, wn + 32 * j, lane) : tr_operand<BN, kBK>(tb, k0, wn + 32 * j, lane);
+#pragma unroll
+      for (int i = 0; i < MI; ++i)
+        ao[c][i] = KROW ? row_operand<BM, kBK>(ta, k0, wm + 32 * i, lane) : tr_operand<BM, kBK>(ta, k0, wm + 32 * i, lane);
+    }
+  };
+
+  // Results.  acc[i][j] holds row 32 i + lane % 32, columns 32 j + 8 (r / 4) + 4 (lane
+  // / 32) + r % 4; 32 rows at a time go through 8 KB of LDS that no load is on its way
+  // to (the last buffers of the rings).  `loaded` runs half way through.
+  float col_bias = 0.0f, col_scale = 1.0f;      // of column wn + lane
+  auto constants = [&](const Place& p) {
+    if constexpr (!F32) {
+      const int n = p.n0 + wn + lane;
+      col_bias = g.e.bias != nullptr && n < g.N ? g.e.bias[n] : 0.0f;
+      col_scale = g.e.w_scale != nullptr && n < g.N ? g.e.w_scale[n] : 1.0f;
+    }
+  };
+  auto epilogue = [&](const Place& p, auto loaded) {
+    float* et = reinterpret_cast<float*>(smem) + (NW == 8 ? (wave < 4 ? 2 : 4) * (TL::kElems / 2) + (wave & 3) * 2048
+                                                  : NW == 4 ? (wave < 2 ? 3 : 7) * (TL::kElems / 2) + (wave & 1) * 2048 : wave * 2048);
+    auto put = [&](const f32x16 (&a)[2]) {
+#pragma unroll
+      for (int j = 0; j < 2; ++j)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const int c = 8 * j + 2 * q + (lane >> 5);
+          *reinterpret_cast<f32x4*>(et + (lane & 31) * 64 + 4 * (c ^ (lane & 15))) =
+              f32x4{a[j][4 * q], a[j][4 * q + 1], a[j][4 * q + 2], a[j][4 * q + 3]};
+        }
+    };
+#pragma unroll 1
+    for (int i = 0; i < MI; ++i) {
+      if (i == MI / 2) loaded();
+      switch (i) {
+        case 0: put(acc[0]); break;
+        case 1: put(acc[1]); break;
+        case 2: put(acc[MI - 2]); break;
+        default: put(acc[MI - 1]);
+      }
+      __builtin_amdgcn_wave_barrier();
+      drain<TO, F32, 32>(g.e, et, col_bias, col_scale, p.m0 + wm + 32 * i, g.M, p.n0 + wn, g.N, p.z);
+      __builtin_amdgcn_wave_barrier();
+    }
+  };
+  // the columns' constants are in registers: nothing later waits for them
+  auto hold_constants = [&]() {
+    if constexpr (!F32) asm volatile("" : "+v"(col_bias), "+v"(col_scale));
+  };
+
   if constexpr (NW != 0) {
-    // bytes from the first to the last element of the tile's operand; where the
-    // contraction runs down columns, to the end of that element's 16-byte
-    // chunk (a load that is not wholly inside reads zeros; the chunk starts inside
-    // the operand at a multiple of 16, and what its rest holds reaches only results
-    // outside the output)
-    const uint32_t size_a = (uint32_t)(KROW ? (rows - 1) * g.lda + 2 * klen : (klen - 1) * g.lda + 2 * ((rows + 7) & ~7));
-    const uint32_t size_b = (uint32_t)(KROW ? (cols - 1) * g.ldb + 2 * klen : (klen - 1) * g.ldb + 2 * ((cols + 7) & ~7));
-    const i32x4 rsa = buffer_rsrc(pa, size_a), rsb = buffer_rsrc(pb, size_b);
+    Stager<BM, KROW, kBK, NT> sa, sb;
+    i32x4 rsa, rsb;
     Mat A = {}, B = {};
     A.ld = (int)(g.lda / 2);
     B.ld = (int)(g.ldb / 2);
-    typedef Tile<BM, KROW, kBK, NT> TL;
-    Stager<BM, KROW, kBK, NT> sa, sb;
-    sa.init(A, 0, rows, 0);
-    sb.init(B, 0, cols, 0);
     const int kba = KROW ? 2 : 2 * A.ld, kbb = KROW ? 2 : 2 * B.ld;   // bytes per contraction index
-    constexpr int kRA = NW == 8 ? 3 : 4;
-    auto issue_a = [&](int s, int st) { sa.load(rsa, lds + st * TL::kElems, s * kBK * kba, klen - s * kBK); };
-    auto issue_b = [&](int s, int st) { sb.load(rsb, lds + (kRA + st) * TL::kElems, s * kBK * kbb, klen - s * kBK); };
-    gemm_stages<T, KROW, W>(lds, nk, acc, issue_a, issue_b);
+    int klen = 0;
+    auto aim = [&](const Place& p) {
+      const int64_t kbeg = (int64_t)p.z * g.kslice;
+      const int rows = (int)min((int64_t)BM, g.M - p.m0), cols = min(BN, g.N - p.n0);
+      const char* pa = g.a + (KROW ? p.m0 * g.lda + 2 * kbeg : kbeg * g.lda + 2 * p.m0);
+      const char* pb = g.b + (KROW ? p.n0 * g.ldb + 2 * kbeg : kbeg * g.ldb + 2 * (int64_t)p.n0);
+      // bytes from the first to the last element of the tile's operand; where the
+      // contraction runs down columns, to the end of that element's 16-byte
+      // chunk (a load that is not wholly inside reads zeros; the chunk starts inside
+      // the operand at a multiple of 16, and what its rest holds reaches only results
+      // outside the output)
+      rsa = buffer_rsrc(pa, (uint32_t)(KROW ? (rows - 1) * g.lda + 2 * p.klen : (p.klen - 1) * g.lda + 2 * ((rows + 7) & ~7)));
+      rsb = buffer_rsrc(pb, (uint32_t)(KROW ? (cols - 1) * g.ldb + 2 * p.klen : (p.klen - 1) * g.ldb + 2 * ((cols + 7) & ~7)));
+      sa.init(A, 0, rows, 0);
+      sb.init(B, 0, cols, 0);
+      klen = p.klen;
+    };
+    auto a_tile = [&](int st) { return lds + st * TL::kElems; };
+    auto b_tile = [&](int st) { return lds + (kRA + st) * TL::kElems; };
+    auto issue_a = [&](int s, int st) { sa.load(rsa, a_tile(st), s * kBK * kba, klen - s * kBK); };
+    auto issue_b = [&](int s, int st) { sb.load(rsb, b_tile(st), s * kBK * kbb, klen - s * kBK); };
+    // the first loads of a tile
+    auto start = [&](const Place& p) {
+      aim(p);
+      if constexpr (NW == 8) {
+        if (p.nk > 0) { issue_a(0, 0); issue_b(0, 0); }
+        if (p.nk > 1) issue_a(1, 1);
+      } else {
+        for (int s = 0; s < 3; ++s)
+          if (s < p.nk) { issue_a(s, s); issue_b(s, s); }
+      }
+    };
+    if (w0 >= wend) return;
+    Place p = place(w0);
+    start(p);
+    bool first = true;
+    while (true) {
+      const int nk = p.nk;
+      clear();
+      if constexpr (NW == 8) {
+        // Turn 4 kt + 2 hf: the first half of the workgroup reads half hf of
+        // stage kt, the second half multiplies what it read in its last turn;
+        // in the next turn they swap.  A stage's buffer is free after turn
+        // 4 kt + 3, so the loads of B's stage kt + 1 (two buffers) go out while
+        // half 0 of stage kt is read, those of A's stage kt + 2 (three) while
+        // half 1 is.
+        const bool second = wave >= NW / 2;
+        if (first) {
+          if (nk > 1) wait_vm<TL::kPer>();
+          else wait_vm<0>();
+        }
+        lds_barrier();
+        constants(p);
+        if (second) lds_barrier();
+        int sa3 = 0;               // kt % 3
+        for (int kt = 0; kt < nk; ++kt) {
+          const bf16* ta = a_tile(sa3);
+          const bf16* tb = b_tile(kt & 1);
+#pragma unroll
+          for (int hf = 0; hf < 2; ++hf) {
+            read_ops(ta, tb, hf);
+            if (hf == 0) {
+              if (kt + 1 < nk) issue_b(kt + 1, (kt + 1) & 1);
+            } else {
+              if (kt + 2 < nk) issue_a(kt + 2, sa3 == 0 ? 2 : sa3 - 1);
+            }
+            auto wait_next = [&]() {     // stage kt + 1 is in LDS (A of stage kt + 2 may be in flight)
+              if (hf == 1) {
+                if (kt + 2 < nk) wait_vm<TL::kPer>();
+                else wait_vm<0>();
+              }
+            };
+            if (second) wait_next();
+            __builtin_amdgcn_sched_barrier(0);
+            lds_barrier();
+            __builtin_amdgcn_sched_barrier(0);
+            __builtin_amdgcn_s_setprio(1);
+            pin(ao);
+            stage_products<T>(acc, ao, bo);
+            pin_sums(acc);
+            __builtin_amdgcn_s_setprio(0);
+            __builtin_amdgcn_sched_barrier(0);
+            if (!second) wait_next();
+            lds_barrier();
+            __builtin_amdgcn_sched_barrier(0);
+          }
+          sa3 = sa3 == 2 ? 0 : sa3 + 1;
+        }
+        if (!second) lds_barrier();
+      } else {
+        constexpr int kLoads = 2 * TL::kPer;
+        for (int kt = 0; kt < nk; ++kt) {
+          const int left = nk - 1 - kt;      // stages after this one
+          if (left >= 2) wait_vm<2 * kLoads>();
+          else if (left == 1) wait_vm<kLoads>();
+          else wait_vm<0>();
+          lds_barrier();     // stage kt is in LDS, and every wave is done with the one before
+          if (kt == 0) constants(p);
+          if (left >= 3) {
+            issue_a(kt + 3, (kt + 3) & 3);
+            issue_b(kt + 3, (kt + 3) & 3);
+          }
+#pragma unroll
+          for (int hf = 0; hf < 2; ++hf) {
+            read_ops(a_tile(kt & 3), b_tile(kt & 3), hf);
+            stage_products<T>(acc, ao, bo);
+          }
+        }
+        lds_barrier();
+      }
+      // every wave is done with the stages
+      hold_constants();
+      w0 += peers;
+      const Place done = p;
+      const bool more = w0 < wend;
+      if (more) {
+        p = place(w0);
+        start(p);
+      }
+      epilogue(done, [&]() { wait_vm<0>(); });
+      if (!more) return;
+      first = false;
+    }
   } else {
-    typedef Tile<kBS, KROW, kBK, 256> TL;
+    const Place p = place(w0);
+    clear();
+    constants(p);
+    const int64_t kbeg = (int64_t)p.z * g.kslice;
+    const int rows = (int)min((int64_t)BM, g.M - p.m0), cols = min(BN, g.N - p.n0);
+    const char* pa = g.a + (KROW ? p.m0 * g.lda + 2 * kbeg : kbeg * g.lda + 2 * p.m0);
+    const char* pb = g.b + (KROW ? p.n0 * g.ldb + 2 * kbeg : kbeg * g.ldb + 2 * (int64_t)p.n0);
     RegStager<KROW, Elem<T>::kBytes> sa, sb;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int wm = (wave / 2) * kWM, wn = (wave % 2) * 64;
-    const int rb = KROW ? g.row_bytes - 2 * kbeg : 0;
-    bf16x8 ao[2][MI], bo[2][2];
-    sa.load(pa, g.lda, rows, 0, klen, rb);
-    sb.load(pb, g.ldb, cols, 0, klen, rb);
+    const int rb = KROW ? (int)(g.row_bytes - 2 * kbeg) : 0;
+    sa.load(pa, g.lda, rows, 0, p.klen, rb);
+    sb.load(pb, g.ldb, cols, 0, p.klen, rb);
     sa.store(lds);
     sb.store(lds + TL::kElems);
     __syncthreads();
-    for (int kt = 0; kt < nk; ++kt) {
-      if (kt + 1 < nk) {
-        sa.load(pa, g.lda, rows, (kt + 1) * kBK, klen, rb);
-        sb.load(pb, g.ldb, cols, (kt + 1) * kBK, klen, rb);
+    for (int kt = 0; kt < p.nk; ++kt) {
+      if (kt + 1 < p.nk) {
+        sa.load(pa, g.lda, rows, (kt + 1) * kBK, p.klen, rb);
+        sb.load(pb, g.ldb, cols, (kt + 1) * kBK, p.klen, rb);
       }
       const bf16* ta = lds + 2 * (kt & 1) * TL::kElems;
-      const bf16* tb = ta + TL::kElems;
 #pragma unroll
       for (int hf = 0; hf < 2; ++hf) {
-#pragma unroll
-        for (int c = 0; c < 2; ++c) {
-          const int k0 = 32 * hf + 16 * c;
-#pragma unroll
-          for (int j = 0; j < 2; ++j)
-            bo[c][j] = KROW ? row_operand<BN, kBK>(tb, k0, wn + 32 * j, lane) : tr_operand<BN, kBK>(tb, k0, wn + 32 * j, lane);
-#pragma unroll
-          for (int i = 0; i < MI; ++i)
-            ao[c][i] = KROW ? row_operand<BM, kBK>(ta, k0, wm + 32 * i, lane) : tr_operand<BM, kBK>(ta, k0, wm + 32 * i, lane);
-        }
+        read_ops(ta, ta + TL::kElems, hf);
         stage_products<T>(acc, ao, bo);
       }
-      if (kt + 1 < nk) {
+      if (kt + 1 < p.nk) {
         bf16* next = lds + 2 * ((kt + 1) & 1) * TL::kElems;
         sa.store(next);
         sb.store(next + TL::kElems);
       }
       __syncthreads();
     }
-  }
-  __syncthreads();   // every wave is done with the stages: their LDS now stages the epilogue
-
-  // 32 rows of the wave's block at a time through its own LDS tile: acc[i][j]
-  // holds rows 32i + 8g + 4h + x (register 4g + x), column 32j + lane % 32;
-  // each lane then handles 8 consecutive columns of rows 8t + lane / 8.
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int wm = (wave / (W / 2)) * kWM, wn = (wave % (W / 2)) * 64;
-  float* et = reinterpret_cast<float*>(smem) + wave * 32 * kEpiS;
-  const int h = lane >> 5, col = lane & 31, er = lane >> 3, ec = (lane & 7) * 8;
-  const int n = n0 + wn + ec, nv = g.N - n;
-  const LinCols lc(F32 ? LinEpi{} : g.e, n, nv);
-#pragma unroll
-  for (int i = 0; i < MI; ++i) {
-#pragma unroll
-    for (int j = 0; j < 2; ++j)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) et[(8 * (r / 4) + 4 * h + (r % 4)) * kEpiS + 32 * j + col] = acc[i][j][r];
-    __builtin_amdgcn_wave_barrier();
-#pragma unroll
-    for (int t = 0; t < 4; ++t) {
-      const int64_t m = m0 + wm + 32 * i + 8 * t + er;
-      float v[8];
-      __builtin_memcpy(v, __builtin_assume_aligned(et + (8 * t + er) * kEpiS + ec, 16), sizeof(v));
-      if (m >= g.M || nv <= 0) continue;
-      if constexpr (F32) store8(g.e.outf + z * g.e.f_slice + m * g.e.f_ld + n, nv, v);
-      else finish8<TO>(g.e, lc, m, n, nv, v);
-    }
-    __builtin_amdgcn_wave_barrier();
+    epilogue(p, [&]() {});
   }
 }
 
@@ -444,8 +566,7 @@ __global__ __launch_bounds__(256) void slices_kernel(const float* __restrict__ p
   if constexpr (F32) {
     store8(e.outf + m * e.f_ld + n, N - n, v);
   } else {
-    const LinCols lc(e, n, N - n);
-    finish8<TO>(e, lc, m, n, N - n, v);
+    finish_row8<TO>(e, lin_cols(e, n, N - n), m, n, N - n, v);
   }
 }
 
@@ -588,8 +709,7 @@ __global__ __launch_bounds__(1024) void skinny_kernel(SkinnyArgs g) {
 #pragma unroll
       for (int i = 0; i < 8; ++i) v[i] += p[i];
     }
-    const LinCols lc(g.e, n, nv);
-    finish8<TO>(g.e, lc, tok, n, nv, v);
+    finish_row8<TO>(g.e, lin_cols(g.e, n, nv), tok, n, nv, v);
   }
 }
 
@@ -727,7 +847,10 @@ hipError_t gemm_launch(GemmArgs g, int ns, hipStream_t st) {
   constexpr size_t lds = (NW == 8 ? 5 : NW == 4 ? 8 : 4) * (size_t)BM * kBK * 2;
   const int64_t tiles = (g.M + BM - 1) / BM * ((g.N + BM - 1) / BM);
   g.kslice = slice_len(g.K, ns);
-  hipLaunchKernelGGL((lin_gemm_kernel<T, TO, KROW, NW, F32>), dim3((unsigned)(tiles * ns)), dim3(NW == 8 ? 512 : 256), lds, st, g);
+  g.work = (int)(tiles * ns);
+  // one workgroup a compute unit is resident with direct loads: they walk the work
+  const int grid = NW == 0 ? g.work : std::min(g.work, kCus);
+  hipLaunchKernelGGL((lin_gemm_kernel<T, TO, KROW, NW, F32>), dim3(grid), dim3(NW == 8 ? 512 : 256), lds, st, g);
   return hipGetLastError();
 }
 
