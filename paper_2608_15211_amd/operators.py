@@ -96,9 +96,9 @@ def _choice(value, choices, name):
 
 
 def _on(t, name, device, dtype):
-    if t.device != device:
-        raise ValueError("%s is on %s, expected %s" % (name, t.device, device))
-    if t.dtype != dtype:
+    if t.get_device() != device:
+        raise ValueError("%s is on %s, expected cuda:%d" % (name, t.device, device))
+    if t.dtype is not dtype:
         raise ValueError("%s has dtype %s, expected %s" % (name, t.dtype, dtype))
 
 
@@ -134,48 +134,63 @@ def _matrix(t, name, device, dtype, rows, cols):
     """(address, row stride) of a rows x cols matrix; (None, 0) for None."""
     if t is None:
         return None, 0
-    _on(t, name, device, dtype)
-    if t.dim() == 0 or t.shape[-1] != cols or t.numel() != rows * cols:
-        raise ValueError("%s has shape %s, expected %d rows of %d" % (name, tuple(t.shape), rows, cols))
-    return t.data_ptr(), _stride(t, name)
+    if t.dtype is not dtype or t.get_device() != device:
+        _on(t, name, device, dtype)
+    shape = t.shape
+    if not shape or shape[-1] != cols or t.numel() != rows * cols:
+        raise ValueError("%s has shape %s, expected %d rows of %d" % (name, tuple(shape), rows, cols))
+    return t.data_ptr(), cols if t.is_contiguous() else _stride(t, name)
 
 
 def _vector(t, name, device, n, dtype=torch.float32):
     if t is None:
         return None
-    _on(t, name, device, dtype)
+    if t.dtype is not dtype or t.get_device() != device:
+        _on(t, name, device, dtype)
     if t.numel() != n or not t.is_contiguous():
         raise ValueError("%s must be contiguous with %d elements" % (name, n))
     return t.data_ptr()
 
 
 def _workspace(ws, need, device):
-    """(tensor, address, bytes)."""
+    """(tensor, address, bytes); need(): bytes to allocate where none is given (the library checks a given one's size)."""
     if ws is None:
-        if need == 0:
+        n = need()
+        if n == 0:
             return None, None, 0
-        ws = torch.empty(need, dtype=torch.uint8, device=device)
-    _on(ws, "workspace", device, torch.uint8)
+        ws = torch.empty(n, dtype=torch.uint8, device="cuda:%d" % device)
+    elif ws.dtype is not torch.uint8 or ws.get_device() != device:
+        _on(ws, "workspace", device, torch.uint8)
     if not ws.is_contiguous():
         raise ValueError("workspace must be contiguous")
     return ws, ws.data_ptr(), ws.numel()
 
 
 def _input(t, name):
+    """The number of its device."""
     if not t.is_cuda:
         raise ValueError("%s must be a device tensor" % name)
     if t.dim() == 0:
         raise ValueError("%s must have a dimension" % name)
-    return t.device
+    return t.get_device()
+
+
+# The current device and a device's current stream as plain numbers: what
+# torch.cuda.current_device() and current_stream().cuda_stream return, without the objects
+# they make on the way (2 us of a call's host time).
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", lambda i: torch.cuda.current_stream(i).cuda_stream)
 
 
 def _call(fn, device, *args):
     """The library's call on the device's current stream."""
-    if device.index == torch.cuda.current_device():
-        _check(fn(*args, torch.cuda.current_stream().cuda_stream))
+    if device == _current_device():
+        status = fn(*args, _raw_stream(device))
     else:
         with torch.cuda.device(device):
-            _check(fn(*args, torch.cuda.current_stream().cuda_stream))
+            status = fn(*args, _raw_stream(device))
+    if status:
+        _check(status)
 
 
 # ---------------------------------------------------- root-mean-square norm
@@ -193,9 +208,9 @@ def terra_rmsnorm_fwd(x, gain=None, res=None, eps=1e-5, out=None, z=None, rstd=N
     if (q is None) != (q_scale is None):
         raise ValueError("q and q_scale come together")
     if z is None and res is not None:
-        z = torch.empty(x.shape, dtype=dt, device=dev)
+        z = torch.empty(x.shape, dtype=dt, device=x.device)
     if out is None and q is None:
-        out = torch.empty(x.shape, dtype=dt, device=dev)
+        out = torch.empty(x.shape, dtype=dt, device=x.device)
     (xp, xl), (rp, rl) = _matrix(x, "x", dev, dt, rows, C), _matrix(res, "res", dev, dt, rows, C)
     (zp, zl), (yp, yl) = _matrix(z, "z", dev, dt, rows, C), _matrix(out, "out", dev, dt, rows, C)
     qp, ql = _matrix(q, "q", dev, torch.float8_e4m3fn, rows, C)
@@ -216,11 +231,10 @@ def terra_rmsnorm_bwd(dy, z, rstd, gain=None, dz=None, out=None, workspace=None)
     dev, dt, C = _input(dy, "dy"), dy.dtype, dy.shape[-1]
     rows = dy.numel() // C if C else 0
     if out is None:
-        out = (torch.empty(dy.shape, dtype=dt, device=dev),
-               None if gain is None else torch.empty(C, dtype=torch.float32, device=dev))
+        out = (torch.empty(dy.shape, dtype=dt, device=dy.device),
+               None if gain is None else torch.empty(C, dtype=torch.float32, device=dy.device))
     dx, dgain = out
-    need = 0 if dgain is None else lib().terra_rmsnorm_bwd_workspace_bytes(rows, C)
-    ws, wp, wn = _workspace(workspace, need, dev)
+    ws, wp, wn = _workspace(workspace, lambda: 0 if dgain is None else lib().terra_rmsnorm_bwd_workspace_bytes(rows, C), dev)
     (yp, yl), (zp, zl) = _matrix(dy, "dy", dev, dt, rows, C), _matrix(z, "z", dev, dt, rows, C)
     (rp, rl), (xp, xl) = _matrix(dz, "dz", dev, dt, rows, C), _matrix(dx, "dx", dev, dt, rows, C)
     _call(lib().terra_rmsnorm_bwd, dev, terra_rmsnorm_desc(rows, C, 0.0, xl, rl, zl, yl, 0), _code(dt), yp, zp,
@@ -250,11 +264,11 @@ def terra_linear_fwd(x, w, bias=None, act="none", res=None, x_scale=None, w_scal
     M = x.numel() // K if K else 0
     to = out_dtype if code == TERRA_E4M3 else dt
     if out is None:
-        out = torch.empty((*x.shape[:-1], N), dtype=to, device=dev)
+        out = torch.empty((*x.shape[:-1], N), dtype=to, device=x.device)
     (xp, xl), (wp, wl) = _matrix(x, "x", dev, dt, M, K), _matrix(w, "w", dev, dt, N, K)
     (yp, yl), (rp, rl) = _matrix(out, "out", dev, to, M, N), _matrix(res, "res", dev, to, M, N)
     pp, pl = _matrix(pre, "pre", dev, to, M, N)
-    ws, sp, sn = _workspace(workspace, lib().terra_linear_fwd_workspace_bytes(M, N, K, code), dev)
+    ws, sp, sn = _workspace(workspace, lambda: lib().terra_linear_fwd_workspace_bytes(M, N, K, code), dev)
     _call(lib().terra_linear_fwd, dev, terra_linear_desc(M, N, K, xl, wl, yl, rl, pl, 0, 0, _choice(act, _ACTS, "act"), _code(to)),
           code, xp, _vector(x_scale, "x_scale", dev, M), wp, _vector(w_scale, "w_scale", dev, N),
           _vector(bias, "bias", dev, N), rp, yp, pp, sp, sn)
@@ -272,13 +286,13 @@ def terra_linear_bwd(dy, x, w, pre=None, act="none", out=None, workspace=None):
     (N, K), code = w.shape, _code(dt)
     M = dy.numel() // N if N else 0
     if out is None:
-        out = (torch.empty((*dy.shape[:-1], K), dtype=dt, device=dev), torch.empty((N, K), dtype=torch.float32, device=dev),
-               torch.empty(N, dtype=torch.float32, device=dev))
+        out = (torch.empty((*dy.shape[:-1], K), dtype=dt, device=dy.device), torch.empty((N, K), dtype=torch.float32, device=dy.device),
+               torch.empty(N, dtype=torch.float32, device=dy.device))
     dx, dw, db = out
     (yp, yl), (xp, xl) = _matrix(dy, "dy", dev, dt, M, N), _matrix(x, "x", dev, dt, M, K)
     (wp, wl), (pp, pl) = _matrix(w, "w", dev, dt, N, K), _matrix(pre, "pre", dev, dt, M, N)
     (ip, il), (gp, gl) = _matrix(dx, "dx", dev, dt, M, K), _matrix(dw, "dw", dev, dt if dw is None or dw.dtype == dt else torch.float32, N, K)
-    ws, sp, sn = _workspace(workspace, lib().terra_linear_bwd_workspace_bytes(M, N, K, code), dev)
+    ws, sp, sn = _workspace(workspace, lambda: lib().terra_linear_bwd_workspace_bytes(M, N, K, code), dev)
     _call(lib().terra_linear_bwd, dev, terra_linear_desc(M, N, K, xl, wl, yl, 0, pl, il, gl, _choice(act, _ACTS, "act"), code), code,
           yp, xp, wp, pp, ip, gp, TERRA_F32 if dw is None else _code(dw.dtype), _vector(db, "dbias", dev, N), sp, sn)
     return out
@@ -299,17 +313,21 @@ def terra_plan_rope(head_dim, rot_dim=None, axes=1, layout="half", base=10000.0,
 
 
 def _heads(x, out, name, tokens, hd, device, dtype):
-    for t, n in ((x, name), (out, name + "'s output")):
-        _on(t, n, device, dtype)
-        if t.dim() < 2 or t.shape[-1] != hd or t.shape != x.shape or t.numel() != tokens * x.shape[-2] * hd:
-            raise ValueError("%s has shape %s, expected (%d tokens, heads, %d)" % (n, tuple(t.shape), tokens, hd))
-        if t.stride(-1) != 1 and hd != 1:
-            raise ValueError("%s must be contiguous along its last dimension" % n)
-    heads = x.shape[-2]
-    if x.is_contiguous() and out.is_contiguous():
-        steps = (heads * hd, hd) * 2
-    else:
-        steps = [s for t in (x, out) for s in (_step(t.shape[:-2], t.stride()[:-2], name) or 0, t.stride(-2))]
+    shape = x.shape
+    for t in (x, out):
+        if t.dtype is not dtype or t.get_device() != device:
+            _on(t, name if t is x else name + "'s output", device, dtype)
+        if t.shape != shape or len(shape) < 2 or shape[-1] != hd or t.numel() != tokens * shape[-2] * hd:
+            raise ValueError("%s has shape %s, expected (%d tokens, heads, %d)" % (name if t is x else name + "'s output", tuple(t.shape), tokens, hd))
+    heads = shape[-2]
+    steps = []
+    for t in (x, out):
+        if t.is_contiguous():
+            steps += (heads * hd, hd)
+        else:
+            if t.stride(-1) != 1:
+                raise ValueError("%s must be contiguous along its last dimension" % (name if t is x else name + "'s output"))
+            steps += (_step(t.shape[:-2], t.stride()[:-2], name) or 0, t.stride(-2))
     return terra_rope_tensor(x.data_ptr(), out.data_ptr(), heads, *steps)
 
 
@@ -319,7 +337,7 @@ def _rope(fn, plan, q, k, pos, grid, out):
         raise ValueError("q has shape %s, expected (tokens, heads, %d)" % (tuple(q.shape), hd))
     tokens = q.numel() // (q.shape[-2] * hd)
     if out is None:
-        out = (torch.empty(q.shape, dtype=dt, device=dev), None if k is None else torch.empty(k.shape, dtype=dt, device=dev))
+        out = (torch.empty(q.shape, dtype=dt, device=q.device), None if k is None else torch.empty(k.shape, dtype=dt, device=q.device))
     tq = _heads(q, out[0], "q", tokens, hd, dev, dt)
     tk = None if k is None else _heads(k, out[1], "k", tokens, hd, dev, dt)
     if pos is not None:
