@@ -76,7 +76,7 @@ struct Rows {
   static constexpr int kPer = kThreads / TPR;     // rows of a workgroup at a time
 };
 
-template <typename T, int TPR, int NCH>
+template <typename T, int TPR, int NCH, bool RAG>
 __global__ __launch_bounds__(Rows<TPR>::kThreads) void rms_fwd_kernel(RmsFwd a) {
   __shared__ float red[16];
   const T* X = (const T*)a.x;
@@ -94,23 +94,35 @@ __global__ __launch_bounds__(Rows<TPR>::kThreads) void rms_fwd_kernel(RmsFwd a) 
 #pragma unroll
       for (int i = 0; i < 8; ++i) g[c][i] = 1.0f;
   }
-  for (int64_t row = (int64_t)blockIdx.x * Rows<TPR>::kPer + threadIdx.x / TPR; row < a.rows; row += step) {
-    float z[NCH][8];
+  // a row's loads go out before the last one is worked on
+  Chunk<T> x[NCH], r[NCH];
+  auto fetch = [&](int64_t row) {
 #pragma unroll
     for (int c = 0; c < NCH; ++c) {
       const int col = 8 * (t + TPR * c);
-      load8(X + row * a.x_ld + col, a.cols - col, z[c]);
+      x[c] = fetch8<RAG>(X + row * a.x_ld + col, a.cols - col);
     }
     if (R != nullptr) {
 #pragma unroll
       for (int c = 0; c < NCH; ++c) {
         const int col = 8 * (t + TPR * c);
-        float r[8];
-        load8(R + row * a.res_ld + col, a.cols - col, r);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) z[c][i] += r[i];
+        r[c] = fetch8<RAG>(R + row * a.res_ld + col, a.cols - col);
       }
     }
+  };
+  int64_t row = (int64_t)blockIdx.x * Rows<TPR>::kPer + threadIdx.x / TPR;
+  if (row < a.rows) fetch(row);
+  for (; row < a.rows; row += step) {
+    float z[NCH][8];
+#pragma unroll
+    for (int c = 0; c < NCH; ++c) widen8(x[c], z[c]);
+    if (R != nullptr) {
+#pragma unroll
+      for (int c = 0; c < NCH; ++c)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) z[c][i] += to_float<T>(r[c].v[i]);
+    }
+    if (row + step < a.rows) fetch(row + step);
     float ss = 0.0f;
 #pragma unroll
     for (int c = 0; c < NCH; ++c)
@@ -120,27 +132,28 @@ __global__ __launch_bounds__(Rows<TPR>::kThreads) void rms_fwd_kernel(RmsFwd a) 
 #pragma unroll
       for (int c = 0; c < NCH; ++c) {
         const int col = 8 * (t + TPR * c);
-        store8(Z + row * a.z_ld + col, a.cols - col, z[c]);
+        put8<RAG>(Z + row * a.z_ld + col, a.cols - col, z[c]);
       }
     }
     const float rstd = 1.0f / sqrtf(row_sum<TPR>(ss, red) / (float)a.cols + a.eps);
     if (a.rstd != nullptr && t == 0) a.rstd[row] = rstd;
-    uint32_t amax = 0;
 #pragma unroll
     for (int c = 0; c < NCH; ++c)
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        z[c][i] = z[c][i] * rstd * g[c][i];
-        amax = max(amax, mag(z[c][i]));
-      }
+      for (int i = 0; i < 8; ++i) z[c][i] = z[c][i] * rstd * g[c][i];
     if (Y != nullptr) {
 #pragma unroll
       for (int c = 0; c < NCH; ++c) {
         const int col = 8 * (t + TPR * c);
-        store8(Y + row * a.y_ld + col, a.cols - col, z[c]);
+        put8<RAG>(Y + row * a.y_ld + col, a.cols - col, z[c]);
       }
     }
     if (a.q != nullptr) {
+      uint32_t amax = 0;
+#pragma unroll
+      for (int c = 0; c < NCH; ++c)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) amax = max(amax, mag(z[c][i]));
       const float s = e4m3_scale(row_max<TPR>(amax, red));
       if (t == 0) a.q_scale[row] = s;
       const float inv = 1.0f / s;
@@ -216,7 +229,7 @@ __global__ __launch_bounds__(1024) void rms_fwd_long_kernel(RmsFwd a) {
 // Backward.  Each wave (or workgroup) walks the rows one grid apart and keeps
 // its share of dgain in registers; the waves of a workgroup add theirs in
 // order through LDS, and the workgroup leaves one row of `part`.
-template <typename T, int TPR, int NCH>
+template <typename T, int TPR, int NCH, bool RAG>
 __global__ __launch_bounds__(Rows<TPR>::kThreads) void rms_bwd_kernel(RmsBwd a) {
   constexpr int kPer = Rows<TPR>::kPer;
   __shared__ float red[16];
@@ -236,15 +249,38 @@ __global__ __launch_bounds__(Rows<TPR>::kThreads) void rms_bwd_kernel(RmsBwd a) 
     if (a.gain != nullptr) load8(a.gain + col, a.cols - col, g[c]);
   }
   const float inv = 1.0f / (float)a.cols;
-  for (int64_t row = (int64_t)blockIdx.x * kPer + threadIdx.x / TPR; row < a.rows; row += step) {
-    float d[NCH][8], zh[NCH][8];
+  // a row's loads go out before the last one is worked on
+  Chunk<T> dy[NCH], zz[NCH], dz[NCH];
+  float rstd_next = 0.0f;
+  auto fetch = [&](int64_t row) {
 #pragma unroll
     for (int c = 0; c < NCH; ++c) {
       const int col = 8 * (t + TPR * c);
-      load8(DY + row * a.dy_ld + col, a.cols - col, d[c]);
-      load8(Z + row * a.z_ld + col, a.cols - col, zh[c]);
+      dy[c] = fetch8<RAG>(DY + row * a.dy_ld + col, a.cols - col);
+      zz[c] = fetch8<RAG>(Z + row * a.z_ld + col, a.cols - col);
     }
-    const float rstd = a.rstd[row];
+    rstd_next = a.rstd[row];
+    if (DZ != nullptr && DX != nullptr) {
+#pragma unroll
+      for (int c = 0; c < NCH; ++c) {
+        const int col = 8 * (t + TPR * c);
+        dz[c] = fetch8<RAG>(DZ + row * a.dz_ld + col, a.cols - col);
+      }
+    }
+  };
+  int64_t row = (int64_t)blockIdx.x * kPer + threadIdx.x / TPR;
+  if (row < a.rows) fetch(row);
+  for (; row < a.rows; row += step) {
+    float d[NCH][8], zh[NCH][8];
+    Chunk<T> r[NCH];
+    const float rstd = rstd_next;
+#pragma unroll
+    for (int c = 0; c < NCH; ++c) {
+      widen8(dy[c], d[c]);
+      widen8(zz[c], zh[c]);
+      r[c] = dz[c];
+    }
+    if (row + step < a.rows) fetch(row + step);
     float s = 0.0f;
 #pragma unroll
     for (int c = 0; c < NCH; ++c)
@@ -260,11 +296,11 @@ __global__ __launch_bounds__(Rows<TPR>::kThreads) void rms_bwd_kernel(RmsBwd a) 
 #pragma unroll
     for (int c = 0; c < NCH; ++c) {
       const int col = 8 * (t + TPR * c);
-      float r[8] = {};
-      if (DZ != nullptr) load8(DZ + row * a.dz_ld + col, a.cols - col, r);
+      float o[8] = {};
+      if (DZ != nullptr) widen8(r[c], o);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) r[i] = fmaf(rstd, fmaf(-zh[c][i], m, d[c][i]), r[i]);
-      store8(DX + row * a.dx_ld + col, a.cols - col, r);
+      for (int i = 0; i < 8; ++i) o[i] = fmaf(rstd, fmaf(-zh[c][i], m, d[c][i]), o[i]);
+      put8<RAG>(DX + row * a.dx_ld + col, a.cols - col, o);
     }
   }
   if (a.part == nullptr) return;
@@ -366,64 +402,74 @@ __global__ __launch_bounds__(1024) void part_sum_kernel(const float* __restrict_
   }
 }
 
-// Threads a row and chunks a thread.  One wave a row up to 2048 columns, where
-// rows are many: a row's sums then need no barrier.  Few rows, and longer
-// ones, take a workgroup each.
+// Threads a row and chunks a thread (one or two: with four the backward's
+// sums, the row and its successor no longer fit the registers).  One wave a row up
+// to 1024 columns, where rows are many: a row's sums then need no barrier.  Few
+// rows, and longer ones, take a workgroup each.  `most`: chunks a thread at
+// 1024 threads, which have 128 registers each.
 struct RowForm {
   int tpr, nch;           // tpr 0: the long form
 };
-RowForm row_form(int64_t rows, int cols) {
+RowForm row_form(int64_t rows, int cols, int most) {
   const int chunks = (cols + 7) / 8;
-  auto pick = [&](int tpr) { return RowForm{tpr, chunks <= tpr ? 1 : chunks <= 2 * tpr ? 2 : 4}; };
-  if (chunks <= 64 || (chunks <= 256 && rows > 1024)) return pick(64);
-  if (chunks <= 512 || (chunks <= 1024 && rows > 256)) return pick(256);
-  if (chunks <= 4096) return pick(1024);
+  auto pick = [&](int tpr) { return RowForm{tpr, chunks <= tpr ? 1 : 2}; };
+  if (chunks <= 64 || (chunks <= 128 && rows > 1024)) return pick(64);
+  if (chunks <= 512) return pick(256);
+  if (chunks <= 1024 * most) return pick(1024);
   return RowForm{0, 0};
 }
+constexpr int kFwdMost = 2, kBwdMost = 1;
 
 }  // namespace
 
-#define TERRA_ROW_FORMS(KERNEL, T)                                                                   \
-  switch (f.tpr + f.nch) {                                                                           \
-    case 65: hipLaunchKernelGGL((KERNEL<T, 64, 1>), grid, dim3(256), 0, st, a); break;               \
-    case 66: hipLaunchKernelGGL((KERNEL<T, 64, 2>), grid, dim3(256), 0, st, a); break;               \
-    case 68: hipLaunchKernelGGL((KERNEL<T, 64, 4>), grid, dim3(256), 0, st, a); break;               \
-    case 257: hipLaunchKernelGGL((KERNEL<T, 256, 1>), grid, dim3(256), 0, st, a); break;             \
-    case 258: hipLaunchKernelGGL((KERNEL<T, 256, 2>), grid, dim3(256), 0, st, a); break;             \
-    case 260: hipLaunchKernelGGL((KERNEL<T, 256, 4>), grid, dim3(256), 0, st, a); break;             \
-    case 1025: hipLaunchKernelGGL((KERNEL<T, 1024, 1>), grid, dim3(1024), 0, st, a); break;          \
-    case 1026: hipLaunchKernelGGL((KERNEL<T, 1024, 2>), grid, dim3(1024), 0, st, a); break;          \
-    case 1028: hipLaunchKernelGGL((KERNEL<T, 1024, 4>), grid, dim3(1024), 0, st, a); break;          \
-  }
+#define TERRA_ROW_FORM(KERNEL, T, TPR, NCH, THREADS)                                            \
+  if (a.cols % 8 == 0) hipLaunchKernelGGL((KERNEL<T, TPR, NCH, false>), grid, dim3(THREADS), 0, st, a); \
+  else hipLaunchKernelGGL((KERNEL<T, TPR, NCH, true>), grid, dim3(THREADS), 0, st, a);           \
+  break
+#define TERRA_ROW_FORMS(KERNEL, T)                              \
+  switch (f.tpr + f.nch) {                                      \
+    case 65: TERRA_ROW_FORM(KERNEL, T, 64, 1, 256);             \
+    case 66: TERRA_ROW_FORM(KERNEL, T, 64, 2, 256);             \
+    case 257: TERRA_ROW_FORM(KERNEL, T, 256, 1, 256);           \
+    case 258: TERRA_ROW_FORM(KERNEL, T, 256, 2, 256);           \
+    case 1025: TERRA_ROW_FORM(KERNEL, T, 1024, 1, 1024);
 
 namespace {
 
-int row_blocks(int64_t rows, int per, int most) {
+// Workgroups: those that are resident at once on 256 compute units walk the rows.
+int row_blocks(int64_t rows, int per, int64_t most) {
   const int64_t b = (rows + per - 1) / per;
   return (int)(b < most ? b : most);
+}
+int row_blocks(int64_t rows, const RowForm& f, bool bwd) {
+  if (f.tpr == 0 || f.tpr == 1024) return row_blocks(rows, 1, 512);
+  return row_blocks(rows, f.tpr == 64 ? 4 : 1, 256 * (f.nch == 2 ? (bwd ? 3 : 5) : (bwd ? 5 : 8)));
 }
 
 template <typename T>
 hipError_t fwd_t(const RmsFwd& a, hipStream_t st) {
-  const RowForm f = row_form(a.rows, a.cols);
-  // enough workgroups for eight waves a SIMD on 256 compute units
-  const dim3 grid(row_blocks(a.rows, f.tpr == 64 ? 4 : 1, f.tpr == 1024 || f.tpr == 0 ? 512 : 2048));
+  const RowForm f = row_form(a.rows, a.cols, kFwdMost);
+  const dim3 grid(row_blocks(a.rows, f, false));
   if (f.tpr == 0) hipLaunchKernelGGL(rms_fwd_long_kernel<T>, grid, dim3(1024), 0, st, a);
   TERRA_ROW_FORMS(rms_fwd_kernel, T)
+    case 1026: TERRA_ROW_FORM(rms_fwd_kernel, T, 1024, 2, 1024);
+  }
   return hipGetLastError();
 }
 
 template <typename T>
 hipError_t bwd_t(const RmsBwd& a, int blocks, hipStream_t st) {
-  const RowForm f = row_form(a.rows, a.cols);
+  const RowForm f = row_form(a.rows, a.cols, kBwdMost);
   const dim3 grid(blocks);
   if (f.tpr == 0) hipLaunchKernelGGL(rms_bwd_long_kernel<T>, grid, dim3(1024), 0, st, a);
   TERRA_ROW_FORMS(rms_bwd_kernel, T)
+  }
   return hipGetLastError();
 }
 
 }  // namespace
 #undef TERRA_ROW_FORMS
+#undef TERRA_ROW_FORM
 
 hipError_t launch_part_sum(const float* part, float* out, int n, int cols, hipStream_t st) {
   hipLaunchKernelGGL(part_sum_kernel, dim3((cols + 31) / 32), dim3(1024), 0, st, part, out, n, cols);
@@ -431,10 +477,7 @@ hipError_t launch_part_sum(const float* part, float* out, int n, int cols, hipSt
 }
 
 // Workgroups of the backward, each with a row of partial sums.
-int rms_bwd_blocks(int64_t rows, int cols) {
-  const RowForm f = row_form(rows, cols);
-  return row_blocks(rows, f.tpr == 64 ? 4 : 1, f.tpr == 1024 || f.tpr == 0 ? 512 : 1024);
-}
+int rms_bwd_blocks(int64_t rows, int cols) { return row_blocks(rows, row_form(rows, cols, kBwdMost), true); }
 
 hipError_t launch_rms_fwd(int dtype, const RmsFwd& a, hipStream_t st) {
   if (a.rows == 0) return hipSuccess;

@@ -20,6 +20,32 @@ struct Chunk {
   T v[8];
 };
 
+// A chunk as it is in memory: elements [0, n) of it, the rest zero.  RAG: n may be
+// anything; else it is at least 8 or the chunk lies outside the row.
+template <bool RAG, typename T>
+__device__ inline Chunk<T> fetch8(const T* p, int n) {
+  Chunk<T> c;
+  if (n >= 8) {
+    __builtin_memcpy(&c, p, sizeof(c));
+  } else {
+    __builtin_memset(&c, 0, sizeof(c));
+    if (RAG && n > 0) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (i < n) c.v[i] = p[i];
+    }
+  }
+  return c;
+}
+template <typename T>
+__device__ inline void widen8(const Chunk<T>& c, float (&f)[8]) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) f[i] = to_float<T>(c.v[i]);
+}
+// Where n >= 8 or the chunk lies outside, or RAG.
+template <bool RAG, typename T>
+__device__ inline void put8(T* p, int n, const float (&f)[8]);
+
 // Elements [0, n) of a chunk (n >= 8: all), the rest zero.
 template <typename T>
 __device__ inline void load8(const T* p, int n, float (&f)[8]) {
@@ -46,6 +72,12 @@ __device__ inline void store8(T* p, int n, const float (&f)[8]) {
     for (int i = 0; i < 8; ++i)
       if (i < n) p[i] = from_float<T>(f[i]);
   }
+}
+
+template <bool RAG, typename T>
+__device__ inline void put8(T* p, int n, const float (&f)[8]) {
+  if (RAG) store8(p, n, f);
+  else if (n >= 8) store8(p, 8, f);
 }
 
 // Eight floats to e4m3, rounded to nearest even; |f| is at most 448 but for
