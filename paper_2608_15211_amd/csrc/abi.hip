@@ -689,10 +689,10 @@ static int check_linear_size(int64_t M, int32_t N, int32_t K) {
   if (M < 0 || N < 1 || K < 1) return fail(TERRA_ERR_INVALID, "M must be >= 0, N and K >= 1");
   if (M >= ((int64_t)1 << 31) - 256 || N > (1 << 28) || K > (1 << 28))
     return fail(TERRA_ERR_UNSUPPORTED, "M must be below 2^31 - 256, N and K at most 2^28");
-  // workgroups of 512 threads, of which a launch takes fewer than 2^32
+  // a launch takes fewer than 2^32 threads: 64 x 64 tiles of 256 of them, at most
   auto tiles = [](int64_t a, int64_t b) { return ((a + 127) / 128) * ((b + 127) / 128); };
-  if (tiles(M, N) >= (1 << 22) || tiles(M, K) >= (1 << 22) || tiles(N, K) >= (1 << 22))
-    return fail(TERRA_ERR_UNSUPPORTED, "a product of 2^22 or more 128 x 128 tiles is not supported");
+  if (tiles(M, N) >= (1 << 21) || tiles(M, K) >= (1 << 21) || tiles(N, K) >= (1 << 21))
+    return fail(TERRA_ERR_UNSUPPORTED, "a product of 2^21 or more 128 x 128 tiles is not supported");
   return ok();
 }
 

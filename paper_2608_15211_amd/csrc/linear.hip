@@ -267,9 +267,8 @@ __device__ __forceinline__ void pin_sums(f32x16 (&acc)[MI][2]) {
     for (int j = 0; j < 2; ++j) asm volatile("" : "+v"(acc[i][j]));
 }
 
-// out[M][N] = sum over k of A(m, k) B(n, k).  NW 8, 4, or 0: four waves with
-// operands through registers.  F32: float32 sums of the slice, else the
-// epilogue.
+// out[M][N] = sum over k of A(m, k) B(n, k).  NW 8: 256 x 256 tiles; 4, 2, 0: 128 x 128
+// tiles of four waves.  F32: float32 sums of the slice, else the epilogue.
 //
 // Work.  There are `work` (slice, tile) pairs; each XCD takes one contiguous run of
 // them, so that tiles sharing operand rows share an L2, and its workgroups take
@@ -278,8 +277,11 @@ __device__ __forceinline__ void pin_sums(f32x16 (&acc)[MI][2]) {
 // each tile.
 // Stages.  The two waves of a SIMD (w and w + 4) take turns: one half of the
 // workgroup multiplies while the other reads its next operands from LDS and
-// issues loads, with a barrier after each turn (eight waves); four waves keep
-// three stages in flight.
+// issues loads, with a barrier after each turn (eight waves); NW 4 keeps
+// three stages in flight, one workgroup a compute unit, for products of a
+// tile or less each; NW 2 holds two stages in half the LDS, so that two workgroups
+// cover each other's waits, for more tiles than that; NW 0 passes operands
+// of any alignment through registers, also two workgroups a unit.
 template <typename T, typename TO, bool KROW, int NW, bool F32>
 __global__ __launch_bounds__(NW == 8 ? 512 : 256, 1) void lin_gemm_kernel(GemmArgs g) {
   constexpr int W = NW == 8 ? 8 : 4, NT = W * 64, BM = NW == 8 ? kBM : kBS, BN = BM;
@@ -287,7 +289,7 @@ __global__ __launch_bounds__(NW == 8 ? 512 : 256, 1) void lin_gemm_kernel(GemmAr
   extern __shared__ __align__(16) char smem[];
   bf16* lds = reinterpret_cast<bf16*>(smem);
   typedef Tile<BM, KROW, kBK, NT> TL;
-  constexpr int kRA = NW == 8 ? 3 : 4;         // stages of A's ring; B's is two (four waves: four)
+  constexpr int kRA = NW == 8 ? 3 : NW == 4 ? 4 : 2;   // stages of A's ring; B's is two (NW 4: four)
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wm = (wave / (W / 2)) * kWM, wn = (wave % (W / 2)) * 64;
@@ -415,7 +417,7 @@ __global__ __launch_bounds__(NW == 8 ? 512 : 256, 1) void lin_gemm_kernel(GemmAr
         if (p.nk > 0) { issue_a(0, 0); issue_b(0, 0); }
         if (p.nk > 1) issue_a(1, 1);
       } else {
-        for (int s = 0; s < 3; ++s)
+        for (int s = 0; s < (NW == 4 ? 3 : 2); ++s)
           if (s < p.nk) { issue_a(s, s); issue_b(s, s); }
       }
     };
@@ -476,6 +478,23 @@ __global__ __launch_bounds__(NW == 8 ? 512 : 256, 1) void lin_gemm_kernel(GemmAr
           sa3 = sa3 == 2 ? 0 : sa3 + 1;
         }
         if (!second) lds_barrier();
+      } else if constexpr (NW == 2) {
+        for (int kt = 0; kt < nk; ++kt) {
+          if (kt + 1 < nk) wait_vm<2 * TL::kPer>();
+          else wait_vm<0>();
+          lds_barrier();     // stage kt is in LDS
+          if (kt == 0) constants(p);
+#pragma unroll
+          for (int hf = 0; hf < 2; ++hf) {
+            read_ops(a_tile(kt & 1), b_tile(kt & 1), hf);
+            stage_products<T>(acc, ao, bo);
+          }
+          lds_barrier();     // every wave is done with it
+          if (kt + 2 < nk) {
+            issue_a(kt + 2, kt & 1);
+            issue_b(kt + 2, kt & 1);
+          }
+        }
       } else {
         constexpr int kLoads = 2 * TL::kPer;
         for (int kt = 0; kt < nk; ++kt) {
@@ -499,6 +518,10 @@ __global__ __launch_bounds__(NW == 8 ? 512 : 256, 1) void lin_gemm_kernel(GemmAr
       }
       // every wave is done with the stages
       hold_constants();
+      if constexpr (NW == 2) {
+        epilogue(p, [&]() {});
+        return;
+      }
       w0 += peers;
       const Place done = p;
       const bool more = w0 < wend;
@@ -674,6 +697,12 @@ __global__ __launch_bounds__(1024) void skinny_kernel(SkinnyArgs g) {
   };
   int it = wave;
   for (; it + (U - 1) * waves < full; it += U * waves) pieces(it, std::integral_constant<int, U>{});
+  if constexpr (U == 4) {
+    if (it + waves < full) {
+      pieces(it, std::integral_constant<int, 2>{});
+      it += 2 * waves;
+    }
+  }
   for (; it < full; it += waves) pieces(it, std::integral_constant<int, 1>{});
   if ((g.row_bytes & 127) != 0 && wave == full % waves) {
     i32x4 a[RT][2], b[MT][2];
@@ -713,6 +742,31 @@ __global__ __launch_bounds__(1024) void skinny_kernel(SkinnyArgs g) {
   }
 }
 
+// Copies of x and w whose rows are whole 16-byte chunks at 16-byte places, zeros behind
+// the row's end: a thread a chunk.
+struct PadArgs {
+  const char* in[2];
+  char* out[2];
+  int64_t ld[2], chunks[2];      // bytes a row of `in`; chunks of `out` altogether
+  int row_bytes, per_row;        // per_row: chunks a row
+};
+template <int ES>
+__global__ __launch_bounds__(256) void pad_rows_kernel(PadArgs a) {
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < a.chunks[0] + a.chunks[1]; i += (int64_t)gridDim.x * 256) {
+    const bool second = i >= a.chunks[0];
+    const int64_t q = second ? i - a.chunks[0] : i, row = q / a.per_row;
+    const int c = (int)(q - row * a.per_row);
+    const i32x4 v = row_tail<ES>(a.in[second] + row * a.ld[second] + 16 * c, a.row_bytes - 16 * c);
+    reinterpret_cast<i32x4*>(a.out[second])[q] = v;
+  }
+}
+template <int ES>
+hipError_t pad_rows(const PadArgs& a, hipStream_t st) {
+  const int64_t blocks = std::min<int64_t>((a.chunks[0] + a.chunks[1] + 255) / 256, 1 << 16);
+  hipLaunchKernelGGL((pad_rows_kernel<ES>), dim3((unsigned)blocks), dim3(256), 0, st, a);
+  return hipGetLastError();
+}
+
 // ---------------------------------------------------------------------------
 // Backward: dt = dy act'(pre), dx = dt W, dW = dt^T x, dbias = sum of dt's rows.
 // ---------------------------------------------------------------------------
@@ -721,31 +775,37 @@ __global__ __launch_bounds__(1024) void skinny_kernel(SkinnyArgs g) {
 // behind the last column), and the column sums of the float32 dt over each of
 // gridDim.y runs of rows.  32 threads along 256 columns, eight rows at a time.
 template <typename T>
-__global__ __launch_bounds__(256) void act_grad_kernel(const T* __restrict__ dy, int64_t dy_ld, const T* __restrict__ pre,
-                                                       int64_t pre_ld, T* __restrict__ dt, int64_t dt_ld,
-                                                       float* __restrict__ part, int64_t M, int N, int64_t run, int act) {
-  __shared__ float red[8][32][9];
+struct ActGrad {
+  const T *dy, *pre;
+  T* dt;
+  float* part;             // [run][N]
+  int64_t dy_ld, pre_ld, dt_ld, M, run;
+  int N, act;
+};
+template <typename T>
+__device__ inline void act_grad_run(const ActGrad<T>& a, int col_block, int64_t run, float (*red)[32][9]) {
   const int c = threadIdx.x & 31, r = threadIdx.x >> 5;
-  const int n = 256 * blockIdx.x + 8 * c, nv = N - n;
-  const int64_t end = min(M, (blockIdx.y + 1) * run);
+  const int n = 256 * col_block + 8 * c, nv = a.N - n;
+  const int64_t end = min(a.M, (run + 1) * a.run);
   float s[8] = {};
   if (nv > 0) {
-    for (int64_t m = blockIdx.y * run + r; m < end; m += 8) {
+#pragma unroll 2
+    for (int64_t m = run * a.run + r; m < end; m += 8) {
       float d[8], t[8];
-      load8(dy + m * dy_ld + n, nv, d);
-      if (act != kActNone) {
-        load8(pre + m * pre_ld + n, nv, t);
-        times_act_grad(d, t, act);
+      load8(a.dy + m * a.dy_ld + n, nv, d);
+      if (a.act != kActNone) {
+        load8(a.pre + m * a.pre_ld + n, nv, t);
+        times_act_grad(d, t, a.act);
         if (nv < 8)
 #pragma unroll
           for (int i = 0; i < 8; ++i) d[i] = i < nv ? d[i] : 0.0f;
       }
 #pragma unroll
       for (int i = 0; i < 8; ++i) s[i] += d[i];
-      if (dt != nullptr) store8(dt + m * dt_ld + n, 8, d);
+      if (a.dt != nullptr) store8(a.dt + m * a.dt_ld + n, 8, d);
     }
   }
-  if (part == nullptr) return;
+  if (a.part == nullptr) return;
 #pragma unroll
   for (int i = 0; i < 8; ++i) red[r][c][i] = s[i];
   __syncthreads();
@@ -753,17 +813,14 @@ __global__ __launch_bounds__(256) void act_grad_kernel(const T* __restrict__ dy,
   float sum = 0.0f;
 #pragma unroll
   for (int k = 0; k < 8; ++k) sum += red[k][col >> 3][col & 7];
-  if (256 * blockIdx.x + col < N) part[(int64_t)blockIdx.y * N + 256 * blockIdx.x + col] = sum;
+  if (256 * col_block + col < a.N) a.part[run * a.N + 256 * col_block + col] = sum;
 }
 
 // out[k][n] = w[n][k] of an N x K matrix, rows of out of whole 16-byte chunks
 // with zeros behind the last column: the data gradient's operand, contracted
 // along memory rows.  64 x 64 tiles.
 template <typename T>
-__global__ __launch_bounds__(256) void transpose_kernel(const T* __restrict__ w, int64_t w_ld, T* __restrict__ out, int64_t out_ld,
-                                                        int N, int K) {
-  __shared__ T tile[64][66];
-  const int n0 = 64 * blockIdx.y, k0 = 64 * blockIdx.x;
+__device__ inline void transpose_tile(const T* w, int64_t w_ld, T* out, int64_t out_ld, int N, int K, int n0, int k0, T (*tile)[66]) {
 #pragma unroll
   for (int u = 0; u < 2; ++u) {
     const int r = (threadIdx.x >> 3) + 32 * u, c = 8 * (threadIdx.x & 7);
@@ -784,6 +841,19 @@ __global__ __launch_bounds__(256) void transpose_kernel(const T* __restrict__ w,
   }
 }
 
+// One launch for both: blocks below `tiles` transpose w (nk tiles along K).
+template <typename T>
+__global__ __launch_bounds__(256) void bwd_prep_kernel(ActGrad<T> a, int col_blocks, const T* w, int64_t w_ld, T* wt, int64_t wt_ld,
+                                                       int K, int tiles, int nk) {
+  __shared__ union {
+    float red[8][32][9];
+    T tile[64][66];
+  } sh;
+  const int b = blockIdx.x;
+  if (b < tiles) return transpose_tile<T>(w, w_ld, wt, wt_ld, a.N, K, 64 * (b / nk), 64 * (b % nk), sh.tile);
+  act_grad_run<T>(a, (b - tiles) % col_blocks, (b - tiles) / col_blocks, sh.red);
+}
+
 // ---------------------------------------------------------------------------
 // Host side.
 // ---------------------------------------------------------------------------
@@ -796,60 +866,62 @@ int64_t up8(int64_t n) { return (n + 7) / 8 * 8; }
 size_t al(size_t n) { return (n + 255) / 256 * 256; }
 int slice_len(int K, int ns) { return ((K + ns - 1) / ns + kBK - 1) / kBK * kBK; }
 
-// Waves of a workgroup (8: 256 x 256 tiles, 4: 128 x 128) and contraction
-// slices, by the time of the slowest compute unit, in us: a stage of 64 units
-// takes 1.35 with eight waves, 0.65 with four, a workgroup 8 and 3 besides; a
-// sum of slices 5 and its traffic.
+// The form of a product (nw: NW of lin_gemm_kernel) and its contraction slices,
+// by the time of the busiest compute unit, in us: a stage of 64 units takes 1.45
+// with eight waves, 0.65 with four, 0.85 for each of two workgroups of form 2,
+// 1.7 through registers (of two workgroups); a workgroup 9 with eight waves and 3 to
+// 4 besides; a sum of slices 5 and its traffic.
 struct Plan {
   int nw, ns;
 };
 double plan_cost(int64_t M, int N, int K, Plan p) {
   const int bm = p.nw == 8 ? kBM : kBS;
   const double tiles = (double)((M + bm - 1) / bm) * ((N + bm - 1) / bm);
-  const double rounds = (double)(int64_t)((tiles * p.ns + kCus - 1) / kCus);
+  const int at_once = p.nw == 0 || p.nw == 2 ? 2 * kCus : kCus;
+  const double rounds = (double)(int64_t)((tiles * p.ns + at_once - 1) / at_once);
   const int stages = slice_len(K, p.ns) / kBK;
   const double sum = p.ns > 1 ? 5.0 + 2e-6 * p.ns * M * N : 0.0;
-  return rounds * (p.nw == 8 ? 1.35 * stages + 8.0 : 0.65 * stages + 3.0) + sum;
+  const double each = p.nw == 8 ? 1.45 * stages + 9.0 : p.nw == 4 ? 0.65 * stages + 3.0 : p.nw == 2 ? 0.85 * stages + 4.0 : 1.7 * stages + 3.0;
+  return rounds * each + sum;
 }
-Plan plan_product(int64_t M, int N, int K, int most, bool eight) {
-  Plan best = {eight ? 8 : 4, 1};
+Plan without_empty(Plan p, int K) {          // slices past the contraction's end
+  const int len = slice_len(K, p.ns);
+  return {p.nw, (K + len - 1) / len};
+}
+// Eight waves in `eights` slices, or one of the others in up to `most`.
+Plan plan_any(int64_t M, int N, int K, int most, int eights, bool direct) {
+  Plan best = {direct ? 8 : 0, direct ? eights : 1};
   double c = plan_cost(M, N, K, best);
-  for (int ns = 1; ns <= most && (ns == 1 || K >= 4 * kBK * ns); ++ns) {
-    const double d = plan_cost(M, N, K, {4, ns});
-    if (d < c) { c = d; best = {4, ns}; }
+  for (int nw : {4, 2, 0}) {
+    if ((nw != 0) != direct) continue;
+    for (int ns = 1; ns <= most && (ns == 1 || K >= 4 * kBK * ns); ++ns) {
+      const double d = plan_cost(M, N, K, {nw, ns});
+      if (d < c) { c = d; best = {nw, ns}; }
+    }
   }
-  const int len = slice_len(K, best.ns);
-  best.ns = (K + len - 1) / len;             // none past the end
-  return best;
+  return without_empty(best, K);
 }
-// A weight gradient over T tokens: token slices for two whole rounds of the
-// eight-wave form, or what the four-wave form does in fewer.
-Plan plan_wgrad(int64_t T, int N, int K, bool eight) {
+Plan plan_product(int64_t M, int N, int K, int most, bool direct) { return plan_any(M, N, K, most, 1, direct); }
+// A weight gradient over T tokens: of the eight-wave form as many token slices as
+// make two whole rounds.
+Plan plan_wgrad(int64_t T, int N, int K, bool direct) {
   const int Ti = (int)std::max<int64_t>(T, 1);
-  Plan best = plan_product(N, K, Ti, kMaxSplit, false);
-  if (eight) {
-    const int64_t tiles = (int64_t)((N + kBM - 1) / kBM) * ((K + kBM - 1) / kBM);
-    int64_t n = std::max<int64_t>(1, 2 * kCus / tiles);
-    n = std::min(n, std::max<int64_t>(1, T / (4 * kBK)));
-    n = std::min<int64_t>(n, kMaxTokenSlices);
-    const Plan p = {8, (int)n};
-    if (plan_cost(N, K, Ti, p) <= plan_cost(N, K, Ti, best)) best = p;
-  }
-  const int len = slice_len(Ti, best.ns);
-  best.ns = (Ti + len - 1) / len;
-  return best;
+  const int64_t tiles = (int64_t)((N + kBM - 1) / kBM) * ((K + kBM - 1) / kBM);
+  int64_t n = std::max<int64_t>(1, 2 * kCus / tiles);
+  n = std::min(n, std::max<int64_t>(1, T / (4 * kBK)));
+  return plan_any(N, K, Ti, kMaxSplit, (int)std::min<int64_t>(n, kMaxTokenSlices), direct);
 }
 
 template <typename T, typename TO, bool KROW, int NW, bool F32>
 hipError_t gemm_launch(GemmArgs g, int ns, hipStream_t st) {
   constexpr int BM = NW == 8 ? kBM : kBS;
   // stages of A and B: 3 + 2 of 32 KB, 4 + 4 of 16 KB, or 2 + 2 of 16 KB
-  constexpr size_t lds = (NW == 8 ? 5 : NW == 4 ? 8 : 4) * (size_t)BM * kBK * 2;
+  constexpr size_t lds = (NW == 8 ? 5 : NW == 4 ? 8 : 4) * (size_t)BM * kBK * 2;   // NW 2 and 0: 64 KB
   const int64_t tiles = (g.M + BM - 1) / BM * ((g.N + BM - 1) / BM);
   g.kslice = slice_len(g.K, ns);
   g.work = (int)(tiles * ns);
   // one workgroup a compute unit is resident with direct loads: they walk the work
-  const int grid = NW == 0 ? g.work : std::min(g.work, kCus);
+  const int grid = NW == 8 || NW == 4 ? std::min(g.work, kCus) : g.work;
   hipLaunchKernelGGL((lin_gemm_kernel<T, TO, KROW, NW, F32>), dim3(grid), dim3(NW == 8 ? 512 : 256), lds, st, g);
   return hipGetLastError();
 }
@@ -862,29 +934,26 @@ bool direct_ok(const void* p, int64_t ld_bytes, int64_t rows) {
 
 // One product of plan p: slices into `part` and their sum, or straight through
 // the epilogue.
+// The form of a plan.
+template <typename T, typename TO, bool KROW, bool F32>
+hipError_t gemm_planned(const GemmArgs& g, Plan p, hipStream_t st) {
+  switch (p.nw) {
+    case 8: return gemm_launch<T, TO, KROW, 8, F32>(g, p.ns, st);
+    case 4: return gemm_launch<T, TO, KROW, 4, F32>(g, p.ns, st);
+    case 2: return gemm_launch<T, TO, KROW, 2, F32>(g, p.ns, st);
+    default: return gemm_launch<T, TO, KROW, 0, F32>(g, p.ns, st);
+  }
+}
+
 template <typename T, typename TO, bool KROW>
-hipError_t product_form(const GemmArgs& g, Plan p, bool direct, bool f32, float* part, hipStream_t st) {
+hipError_t product_form(const GemmArgs& g, Plan p, bool f32, float* part, hipStream_t st) {
   GemmArgs s = g;
   if (p.ns > 1) {
     s.e.outf = part;
     s.e.f_ld = up8(g.N);
     s.e.f_slice = g.M * s.e.f_ld;
   }
-  hipError_t e;
-  if (f32 || p.ns > 1) {
-    if constexpr (!KROW) {
-      e = !direct ? gemm_launch<T, TO, KROW, 0, true>(s, p.ns, st)
-          : p.nw == 8 ? gemm_launch<T, TO, KROW, 8, true>(s, p.ns, st)
-                      : gemm_launch<T, TO, KROW, 4, true>(s, p.ns, st);
-    } else {
-      // forward slices are taken by the four-wave forms only
-      e = direct ? gemm_launch<T, TO, KROW, 4, true>(s, p.ns, st) : gemm_launch<T, TO, KROW, 0, true>(s, p.ns, st);
-    }
-  } else {
-    e = !direct ? gemm_launch<T, TO, KROW, 0, false>(s, 1, st)
-        : p.nw == 8 ? gemm_launch<T, TO, KROW, 8, false>(s, 1, st)
-                    : gemm_launch<T, TO, KROW, 4, false>(s, 1, st);
-  }
+  const hipError_t e = f32 || p.ns > 1 ? gemm_planned<T, TO, KROW, true>(s, p, st) : gemm_planned<T, TO, KROW, false>(s, p, st);
   if (e != hipSuccess || p.ns == 1) return e;
   const int64_t n = g.M * ((g.N + 7) / 8);
   const dim3 grid((unsigned)((n + 255) / 256));
@@ -916,26 +985,57 @@ hipError_t row_product(GemmArgs g, float* part, hipStream_t st) {
     if (whole > 0 && whole < nM) {
       GemmArgs first = g;
       first.M = whole * kBM;
-      const hipError_t e = product_form<T, TO, true>(first, Plan{8, 1}, true, false, nullptr, st);
+      const hipError_t e = product_form<T, TO, true>(first, Plan{8, 1}, false, nullptr, st);
       if (e != hipSuccess) return e;
       skip_rows<TO>(g, first.M);
-      p = plan_product(g.M, g.N, g.K, 1, true);
+      p = plan_product(g.M, g.N, g.K, 1, true);             // no slices: `part` may not hold them
     }
   }
-  return product_form<T, TO, true>(g, p, direct, false, part, st);
+  return product_form<T, TO, true>(g, p, false, part, st);
 }
 
 template <typename T, typename TO, int MT>
 hipError_t skinny_rt(const SkinnyArgs& g, hipStream_t st) {
   const int its = (g.row_bytes + 127) / 128;
   const int rt = (g.N + 15) / 16 >= 4 * kCus ? 2 : 1;
+  // four pieces a wave, whose loads go out together, while there are 16 waves
   int waves = 16;
-  while (waves > 1 && waves * 2 > its) waves /= 2;
+  while (waves > 4 && waves * 4 > its) waves /= 2;
+  while (waves > 1 && waves > its) waves /= 2;
   const dim3 grid((g.N + 16 * rt - 1) / (16 * rt));
   const size_t lds = (size_t)waves * MT * rt * 16 * kRedS * sizeof(float);
   if (rt == 2) hipLaunchKernelGGL((skinny_kernel<T, TO, MT, 2>), grid, dim3(64 * waves), lds, st, g);
   else hipLaunchKernelGGL((skinny_kernel<T, TO, MT, 1>), grid, dim3(64 * waves), lds, st, g);
   return hipGetLastError();
+}
+
+size_t split_floats(int64_t M, int N, int K, bool direct) {
+  const Plan p = plan_product(M, N, K, kMaxSplit, direct);
+  return p.ns > 1 ? (size_t)p.ns * M * up8(N) : 0;
+}
+// Forward workspace, from the sizes alone: slices, and where rows are no whole chunks
+// and the copies pay (10 us and their traffic against the form through
+// registers) the padded x and w.
+struct FwdWs {
+  size_t x, w, total;
+  bool padded;
+};
+FwdWs fwd_ws(int64_t M, int N, int row_bytes) {
+  FwdWs w = {};
+  const int ku = (row_bytes + 1) / 2, pad = (row_bytes + 15) / 16 * 16;
+  size_t off = 4 * std::max(split_floats(M, N, ku, true), split_floats(M, N, ku, false));
+  if (row_bytes % 16 != 0) {
+    const double copy = 10.0 + 2.0 * (M + N) * pad / 4e6;
+    w.padded = plan_cost(M, N, pad / 2, plan_product(M, N, pad / 2, kMaxSplit, true)) + copy <
+               plan_cost(M, N, ku, plan_product(M, N, ku, kMaxSplit, false));
+  }
+  if (w.padded) {
+    off = al(std::max(off, 4 * split_floats(M, N, pad / 2, true)));
+    w.x = off; off += al((size_t)M * pad);
+    w.w = off; off += al((size_t)N * pad);
+  }
+  w.total = off;
+  return w;
 }
 
 template <typename T, typename TO>
@@ -951,19 +1051,26 @@ hipError_t fwd_t(const LinFwd& a, void* ws, hipStream_t st) {
   GemmArgs g = {};
   g.a = (const char*)a.x; g.b = (const char*)a.w; g.lda = a.x_ld * ES; g.ldb = a.w_ld * ES;
   g.M = a.M; g.N = a.N; g.row_bytes = a.K * ES; g.K = (g.row_bytes + 1) / 2; g.e = e;
+  const FwdWs w = fwd_ws(a.M, a.N, g.row_bytes);
+  if (w.padded) {
+    PadArgs p = {{g.a, g.b}, {(char*)ws + w.x, (char*)ws + w.w}, {g.lda, g.ldb}, {}, g.row_bytes, (g.row_bytes + 15) / 16};
+    p.chunks[0] = a.M * p.per_row;
+    p.chunks[1] = (int64_t)a.N * p.per_row;
+    const hipError_t copied = pad_rows<ES>(p, st);
+    if (copied != hipSuccess) return copied;
+    g.a = p.out[0]; g.b = p.out[1];
+    g.lda = g.ldb = g.row_bytes = 16 * p.per_row;
+    g.K = g.row_bytes / 2;
+  }
   return row_product<T, TO>(g, (float*)ws, st);
 }
 
 // Backward workspace: dt, the transposed W, slices of either product, column sums.
 struct BwdWs {
-  size_t dt, wt, part, sums, total;
+  size_t dt, wt, x, part, sums, total;
   int64_t dt_ld, run;
   int runs;
 };
-size_t split_floats(int64_t M, int N, int K, bool eight) {
-  const Plan p = plan_product(M, N, K, kMaxSplit, eight);
-  return p.ns > 1 ? (size_t)p.ns * M * up8(N) : 0;
-}
 BwdWs bwd_ws(int64_t M, int N, int K) {
   BwdWs w;
   w.dt_ld = up8(N);
@@ -978,6 +1085,7 @@ BwdWs bwd_ws(int64_t M, int N, int K) {
   size_t off = 0;
   w.dt = off; off += al((size_t)M * w.dt_ld * 2);
   w.wt = off; off += al((size_t)K * w.dt_ld * 2);
+  w.x = off; off += K % 8 != 0 ? al((size_t)M * up8(K) * 2) : 0;
   w.part = off; off += al(part * 4);
   w.sums = off; off += al((size_t)w.runs * N * 4);
   w.total = off;
@@ -991,21 +1099,25 @@ hipError_t bwd_t(const LinBwd& a, char* ws, hipStream_t st) {
   const bool need_dt = (a.dx != nullptr || a.dw != nullptr) &&
                        (a.act != kActNone || a.N % 8 != 0 || !direct_ok(a.dy, a.dy_ld * 2, kBM));
   T* dt = need_dt ? (T*)(ws + w.dt) : nullptr;
-  float* sums = a.db != nullptr ? (float*)(ws + w.sums) : nullptr;
-  if (need_dt || sums != nullptr) {
-    hipLaunchKernelGGL((act_grad_kernel<T>), dim3((a.N + 255) / 256, w.runs), dim3(256), 0, st, (const T*)a.dy, a.dy_ld,
-                       (const T*)a.pre, a.pre_ld, dt, w.dt_ld, sums, a.M, a.N, w.run, a.act);
-    if ((e = hipGetLastError()) != hipSuccess) return e;
+  T* wt = (T*)(ws + w.wt);
+  // one run of rows: its sums are dbias
+  float* sums = a.db == nullptr ? nullptr : w.runs == 1 ? a.db : (float*)(ws + w.sums);
+  {
+    const int nk = (a.K + 63) / 64;
+    const int tiles = a.dx != nullptr && a.M > 0 ? nk * (int)((w.dt_ld + 63) / 64) : 0;
+    const int col_blocks = (a.N + 255) / 256, blocks = need_dt || sums != nullptr ? col_blocks * w.runs : 0;
+    if (tiles + blocks > 0) {
+      const ActGrad<T> g = {(const T*)a.dy, (const T*)a.pre, dt, sums, a.dy_ld, a.pre_ld, w.dt_ld, a.M, w.run, a.N, a.act};
+      hipLaunchKernelGGL((bwd_prep_kernel<T>), dim3(tiles + blocks), dim3(256), 0, st, g, col_blocks, (const T*)a.w, a.w_ld, wt, w.dt_ld,
+                         a.K, tiles, nk);
+      if ((e = hipGetLastError()) != hipSuccess) return e;
+    }
   }
-  if (sums != nullptr && (e = launch_part_sum(sums, a.db, w.runs, a.N, st)) != hipSuccess) return e;
+  if (sums != nullptr && w.runs > 1 && (e = launch_part_sum(sums, a.db, w.runs, a.N, st)) != hipSuccess) return e;
   const char* d = need_dt ? (const char*)dt : (const char*)a.dy;
   const int64_t d_ld = 2 * (need_dt ? w.dt_ld : a.dy_ld);
   float* part = (float*)(ws + w.part);
   if (a.dx != nullptr && a.M > 0) {
-    T* wt = (T*)(ws + w.wt);
-    hipLaunchKernelGGL((transpose_kernel<T>), dim3((a.K + 63) / 64, (unsigned)((w.dt_ld + 63) / 64)), dim3(256), 0, st, (const T*)a.w,
-                       a.w_ld, wt, w.dt_ld, a.N, a.K);
-    if ((e = hipGetLastError()) != hipSuccess) return e;
     GemmArgs g = {};
     g.a = d; g.lda = d_ld; g.b = (const char*)wt; g.ldb = 2 * w.dt_ld;
     g.M = a.M; g.N = a.K; g.K = (int)w.dt_ld; g.row_bytes = 2 * (int)w.dt_ld;
@@ -1019,10 +1131,16 @@ hipError_t bwd_t(const LinBwd& a, char* ws, hipStream_t st) {
     if (a.dw_f32) { g.e.outf = (float*)a.dw; g.e.f_ld = a.dw_ld; }
     else { g.e.y = a.dw; g.e.y_ld = a.dw_ld; }
     Plan p = plan_wgrad(a.M, a.N, a.K, true);
+    if (a.K % 8 != 0 && a.M > 0) {             // rows of whole chunks (the copy: a pass over x)
+      PadArgs q = {{g.b, nullptr}, {ws + w.x, nullptr}, {g.ldb, 0}, {}, 2 * a.K, (a.K + 7) / 8};
+      q.chunks[0] = a.M * q.per_row;
+      if ((e = pad_rows<2>(q, st)) != hipSuccess) return e;
+      g.b = ws + w.x; g.ldb = 16 * q.per_row;
+    }
     const int64_t rows = slice_len(g.K, p.ns);
     const bool direct = direct_ok(g.a, g.lda, rows) && direct_ok(g.b, g.ldb, rows);
     if (!direct) p = plan_wgrad(a.M, a.N, a.K, false);
-    if ((e = product_form<T, T, false>(g, p, direct, a.dw_f32, part, st)) != hipSuccess) return e;
+    if ((e = product_form<T, T, false>(g, p, a.dw_f32, part, st)) != hipSuccess) return e;
   }
   return hipSuccess;
 }
@@ -1031,8 +1149,7 @@ hipError_t bwd_t(const LinBwd& a, char* ws, hipStream_t st) {
 
 size_t lin_fwd_workspace(int64_t M, int N, int K, int dtype) {
   if (M <= kSkinnyMost) return 0;
-  const int ku = dtype == kE4m3 ? (K + 1) / 2 : K;
-  return 4 * std::max(split_floats(M, N, ku, true), split_floats(M, N, ku, false));
+  return fwd_ws(M, N, dtype == kE4m3 ? K : 2 * K).total;
 }
 size_t lin_bwd_workspace(int64_t M, int N, int K) { return bwd_ws(M, N, K).total; }
 
