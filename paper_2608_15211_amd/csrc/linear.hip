@@ -163,13 +163,12 @@ __device__ inline LinCols lin_cols(const LinEpi& e, int n, int nv) {
   return c;
 }
 
-// Columns [n, n + 8) (nv of them inside) of row m.
+// Columns [n, n + 8) (nv of them inside) of row m, whose scale is xs.
 template <typename TO>
-__device__ __forceinline__ void finish_row8(const LinEpi& e, const LinCols& c, int64_t m, int n, int nv, float (&v)[8]) {
+__device__ __forceinline__ void finish8(const LinEpi& e, const LinCols& c, float xs, int64_t m, int n, int nv, float (&v)[8]) {
   float res[8];
   if (e.res != nullptr) load8((const TO*)e.res + m * e.res_ld + n, nv, res);
   if (e.x_scale != nullptr) {
-    const float xs = e.x_scale[m];
 #pragma unroll
     for (int i = 0; i < 8; ++i) v[i] = fmaf(v[i] * xs, c.scale[i], c.bias[i]);
   } else {
@@ -185,6 +184,11 @@ __device__ __forceinline__ void finish_row8(const LinEpi& e, const LinCols& c, i
   store8((TO*)e.y + m * e.y_ld + n, nv, v);
 }
 
+template <typename TO>
+__device__ inline void finish_row8(const LinEpi& e, const LinCols& c, int64_t m, int n, int nv, float (&v)[8]) {
+  finish8<TO>(e, c, e.x_scale != nullptr ? e.x_scale[m] : 1.0f, m, n, nv, v);
+}
+
 // A wave's results on their way out: ROWS x 64 float32 in its part of LDS, 16-byte
 // chunk c of row m at chunk c ^ (m % 16) (writes of a lane's own rows and reads of
 // whole rows then hit every bank once).  A lane takes 8 columns of rows 8 t + lane / 8,
@@ -193,8 +197,8 @@ __device__ __forceinline__ void finish_row8(const LinEpi& e, const LinCols& c, i
 // the loop for every block of a tile: unrolled over them the code no longer fits
 // the instruction cache (an epilogue of 22 us a tile).
 template <typename TO, bool F32, int ROWS>
-__device__ __forceinline__ void drain(const LinEpi& e, const float* et, float col_bias, float col_scale, int64_t m0, int64_t M, int n0,
-                                      int N, int z) {
+__device__ __forceinline__ void drain(const LinEpi& e, const float* et, float col_bias, float col_scale, float row_scale, int lane0,
+                                      int64_t m0, int64_t M, int n0, int N, int z) {
   const int lane = threadIdx.x & 63, er = lane >> 3, ec = lane & 7;
   const int n = n0 + 8 * ec, nv = N - n;
   LinCols lc;
@@ -216,11 +220,14 @@ __device__ __forceinline__ void drain(const LinEpi& e, const float* et, float co
       const f32x4 lo = *reinterpret_cast<const f32x4*>(et + row * 64 + 4 * ((2 * ec) ^ (row & 15)));
       const f32x4 hi = *reinterpret_cast<const f32x4*>(et + row * 64 + 4 * ((2 * ec + 1) ^ (row & 15)));
       float v[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
-      if (!kWhole && (m >= M || nv <= 0)) continue;
+      const bool in = kWhole || (m < M && nv > 0);
       if constexpr (F32) {
+        if (!in) continue;
         store8(e.outf + z * e.f_slice + m * e.f_ld + n, left, v);
       } else {
-        finish_row8<TO>(e, lc, m, n, left, v);
+        // the row's scale is lane lane0 + row's: a load here would wait for all that go before it
+        const float xs = e.x_scale != nullptr ? __shfl(row_scale, lane0 + row, 64) : 1.0f;
+        if (in) finish8<TO>(e, lc, xs, m, n, left, v);
       }
     }
   };
@@ -267,7 +274,7 @@ __device__ __forceinline__ void pin_sums(f32x16 (&acc)[MI][2]) {
     for (int j = 0; j < 2; ++j) asm volatile("" : "+v"(acc[i][j]));
 }
 
-// out[M][N] = sum over k of A(m, k) B(n, k).  NW 8: 256 x 256 tiles; 4, 2, 0: 128 x 128
+// out[M][N] = sum over k of A(m, k) B(n, k).  NW 8: 256 x 256 tiles; 2 and 0: 128 x 128
 // tiles of four waves.  F32: float32 sums of the slice, else the epilogue.
 //
 // Work.  There are `work` (slice, tile) pairs; each XCD takes one contiguous run of
@@ -277,11 +284,11 @@ __device__ __forceinline__ void pin_sums(f32x16 (&acc)[MI][2]) {
 // each tile.
 // Stages.  The two waves of a SIMD (w and w + 4) take turns: one half of the
 // workgroup multiplies while the other reads its next operands from LDS and
-// issues loads, with a barrier after each turn (eight waves); NW 4 keeps
-// three stages in flight, one workgroup a compute unit, for products of a
-// tile or less each; NW 2 holds two stages in half the LDS, so that two workgroups
-// cover each other's waits, for more tiles than that; NW 0 passes operands
-// of any alignment through registers, also two workgroups a unit.
+// issues loads, with a barrier after each turn (NW 8); NW 2 holds two stages in
+// 64 KB, so that two workgroups a unit cover each other's waits (one
+// workgroup with three stages in flight: 1441 x 4928 x 1856 in 46.8 us against
+// 36.9, up to one tile a unit within 2 % of this); NW 0 passes operands of
+// any alignment through registers.
 template <typename T, typename TO, bool KROW, int NW, bool F32>
 __global__ __launch_bounds__(NW == 8 ? 512 : 256, 1) void lin_gemm_kernel(GemmArgs g) {
   constexpr int W = NW == 8 ? 8 : 4, NT = W * 64, BM = NW == 8 ? kBM : kBS, BN = BM;
@@ -289,7 +296,7 @@ __global__ __launch_bounds__(NW == 8 ? 512 : 256, 1) void lin_gemm_kernel(GemmAr
   extern __shared__ __align__(16) char smem[];
   bf16* lds = reinterpret_cast<bf16*>(smem);
   typedef Tile<BM, KROW, kBK, NT> TL;
-  constexpr int kRA = NW == 8 ? 3 : NW == 4 ? 4 : 2;   // stages of A's ring; B's is two (NW 4: four)
+  constexpr int kRA = NW == 8 ? 3 : 2;         // stages of A's ring; B's is two
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wm = (wave / (W / 2)) * kWM, wn = (wave % (W / 2)) * 64;
@@ -342,17 +349,25 @@ __global__ __launch_bounds__(NW == 8 ? 512 : 256, 1) void lin_gemm_kernel(GemmAr
   // Results.  acc[i][j] holds row 32 i + lane % 32, columns 32 j + 8 (r / 4) + 4 (lane
   // / 32) + r % 4; 32 rows at a time go through 8 KB of LDS that no load is on its way
   // to (the last buffers of the rings).  `loaded` runs half way through.
-  float col_bias = 0.0f, col_scale = 1.0f;      // of column wn + lane
+  constexpr int kRS = kWM / 64;
+  constexpr bool kScaled = std::is_same<T, e4m3>::value && !F32;
+  float col_bias = 0.0f, col_scale = 1.0f, row_scale[kRS];      // of column wn + lane, of rows wm + 64 r + lane
   auto constants = [&](const Place& p) {
     if constexpr (!F32) {
       const int n = p.n0 + wn + lane;
       col_bias = g.e.bias != nullptr && n < g.N ? g.e.bias[n] : 0.0f;
       col_scale = g.e.w_scale != nullptr && n < g.N ? g.e.w_scale[n] : 1.0f;
+      if constexpr (kScaled) {
+#pragma unroll
+        for (int r = 0; r < kRS; ++r) {
+          const int64_t m = p.m0 + wm + 64 * r + lane;
+          row_scale[r] = m < g.M ? g.e.x_scale[m] : 0.0f;
+        }
+      }
     }
   };
   auto epilogue = [&](const Place& p, auto loaded) {
-    float* et = reinterpret_cast<float*>(smem) + (NW == 8 ? (wave < 4 ? 2 : 4) * (TL::kElems / 2) + (wave & 3) * 2048
-                                                  : NW == 4 ? (wave < 2 ? 3 : 7) * (TL::kElems / 2) + (wave & 1) * 2048 : wave * 2048);
+    float* et = reinterpret_cast<float*>(smem) + (NW == 8 ? (wave < 4 ? 2 : 4) * (TL::kElems / 2) + (wave & 3) * 2048 : wave * 2048);
     auto put = [&](const f32x16 (&a)[2]) {
 #pragma unroll
       for (int j = 0; j < 2; ++j)
@@ -373,13 +388,17 @@ __global__ __launch_bounds__(NW == 8 ? 512 : 256, 1) void lin_gemm_kernel(GemmAr
         default: put(acc[MI - 1]);
       }
       __builtin_amdgcn_wave_barrier();
-      drain<TO, F32, 32>(g.e, et, col_bias, col_scale, p.m0 + wm + 32 * i, g.M, p.n0 + wn, g.N, p.z);
+      drain<TO, F32, 32>(g.e, et, col_bias, col_scale, kScaled ? row_scale[kRS == 2 ? i >> 1 : 0] : 0.0f, 32 * (i & 1), p.m0 + wm + 32 * i, g.M, p.n0 + wn, g.N, p.z);
       __builtin_amdgcn_wave_barrier();
     }
   };
   // the columns' constants are in registers: nothing later waits for them
   auto hold_constants = [&]() {
     if constexpr (!F32) asm volatile("" : "+v"(col_bias), "+v"(col_scale));
+    if constexpr (kScaled) {
+#pragma unroll
+      for (int r = 0; r < kRS; ++r) asm volatile("" : "+v"(row_scale[r]));
+    }
   };
 
   if constexpr (NW != 0) {
@@ -417,7 +436,7 @@ __global__ __launch_bounds__(NW == 8 ? 512 : 256, 1) void lin_gemm_kernel(GemmAr
         if (p.nk > 0) { issue_a(0, 0); issue_b(0, 0); }
         if (p.nk > 1) issue_a(1, 1);
       } else {
-        for (int s = 0; s < (NW == 4 ? 3 : 2); ++s)
+        for (int s = 0; s < 2; ++s)
           if (s < p.nk) { issue_a(s, s); issue_b(s, s); }
       }
     };
@@ -478,7 +497,7 @@ __global__ __launch_bounds__(NW == 8 ? 512 : 256, 1) void lin_gemm_kernel(GemmAr
           sa3 = sa3 == 2 ? 0 : sa3 + 1;
         }
         if (!second) lds_barrier();
-      } else if constexpr (NW == 2) {
+      } else {
         for (int kt = 0; kt < nk; ++kt) {
           if (kt + 1 < nk) wait_vm<2 * TL::kPer>();
           else wait_vm<0>();
@@ -495,26 +514,6 @@ __global__ __launch_bounds__(NW == 8 ? 512 : 256, 1) void lin_gemm_kernel(GemmAr
             issue_b(kt + 2, kt & 1);
           }
         }
-      } else {
-        constexpr int kLoads = 2 * TL::kPer;
-        for (int kt = 0; kt < nk; ++kt) {
-          const int left = nk - 1 - kt;      // stages after this one
-          if (left >= 2) wait_vm<2 * kLoads>();
-          else if (left == 1) wait_vm<kLoads>();
-          else wait_vm<0>();
-          lds_barrier();     // stage kt is in LDS, and every wave is done with the one before
-          if (kt == 0) constants(p);
-          if (left >= 3) {
-            issue_a(kt + 3, (kt + 3) & 3);
-            issue_b(kt + 3, (kt + 3) & 3);
-          }
-#pragma unroll
-          for (int hf = 0; hf < 2; ++hf) {
-            read_ops(a_tile(kt & 3), b_tile(kt & 3), hf);
-            stage_products<T>(acc, ao, bo);
-          }
-        }
-        lds_barrier();
       }
       // every wave is done with the stages
       hold_constants();
@@ -868,60 +867,87 @@ int slice_len(int K, int ns) { return ((K + ns - 1) / ns + kBK - 1) / kBK * kBK;
 
 // The form of a product (nw: NW of lin_gemm_kernel) and its contraction slices,
 // by the time of the busiest compute unit, in us: a stage of 64 units takes 1.45
-// with eight waves, 0.65 with four, 0.85 for each of two workgroups of form 2,
-// 1.7 through registers (of two workgroups); a workgroup 9 with eight waves and 3 to
-// 4 besides; a sum of slices 5 and its traffic.
+// with eight waves; in form 2 0.65 for one workgroup on a unit and 1.05 for each
+// of two; through registers 1.7 (of two); a workgroup 9 with eight waves and 3
+// to 4 besides; a sum of slices 5 and its traffic.  Measured in one slice, eight
+// waves and form 2 (bf16, M x N x K): 2048 x 2048 x 1024 28.2 and 17.3 us, 4096
+// x 2048 x 512 21.9 and 16.4, 1441 x 4928 x 1856 46.8 and 36.9, 4096 x 4096 x
+// 1024 36.2 and 42.3, 8192 x 2048 x 2048 59 and 72, 34560 x 1024 x 4096 295
+// and 318 (266 as whole rounds of eight waves and the rest in form 2).
 struct Plan {
   int nw, ns;
 };
 double plan_cost(int64_t M, int N, int K, Plan p) {
   const int bm = p.nw == 8 ? kBM : kBS;
-  const double tiles = (double)((M + bm - 1) / bm) * ((N + bm - 1) / bm);
-  const int at_once = p.nw == 0 || p.nw == 2 ? 2 * kCus : kCus;
-  const double rounds = (double)(int64_t)((tiles * p.ns + at_once - 1) / at_once);
+  const double work = (double)((M + bm - 1) / bm) * ((N + bm - 1) / bm) * p.ns;
+  const bool pairs = p.nw == 0 || (p.nw == 2 && work > kCus);      // two workgroups a unit at once
+  const double rounds = (double)(int64_t)((work + (pairs ? 2 : 1) * kCus - 1) / ((pairs ? 2 : 1) * kCus));
   const int stages = slice_len(K, p.ns) / kBK;
-  const double sum = p.ns > 1 ? 5.0 + 2e-6 * p.ns * M * N : 0.0;
-  const double each = p.nw == 8 ? 1.45 * stages + 9.0 : p.nw == 4 ? 0.65 * stages + 3.0 : p.nw == 2 ? 0.85 * stages + 4.0 : 1.7 * stages + 3.0;
+  const double sum = p.ns > 1 ? 5.0 + 0.8e-6 * p.ns * M * N : 0.0;
+  const double each = p.nw == 8 ? 1.45 * stages + 9.0 : p.nw == 0 ? 1.7 * stages + 3.0 : pairs ? 1.05 * stages + 4.0 : 0.65 * stages + 3.0;
   return rounds * each + sum;
 }
 Plan without_empty(Plan p, int K) {          // slices past the contraction's end
   const int len = slice_len(K, p.ns);
   return {p.nw, (K + len - 1) / len};
 }
-// Eight waves in `eights` slices, or one of the others in up to `most`.
-Plan plan_any(int64_t M, int N, int K, int most, int eights, bool direct) {
-  Plan best = {direct ? 8 : 0, direct ? eights : 1};
-  double c = plan_cost(M, N, K, best);
-  for (int nw : {4, 2, 0}) {
+// The best of the other forms in up to `most` slices, and its time.
+double plan_small(int64_t M, int N, int K, int most, bool direct, Plan* best) {
+  double c = 1e30;
+  for (int nw : {2, 0}) {
     if ((nw != 0) != direct) continue;
     for (int ns = 1; ns <= most && (ns == 1 || K >= 4 * kBK * ns); ++ns) {
       const double d = plan_cost(M, N, K, {nw, ns});
-      if (d < c) { c = d; best = {nw, ns}; }
+      if (d < c) { c = d; *best = {nw, ns}; }
     }
+  }
+  return c;
+}
+// Rows that eight waves take in whole rounds of one tile a compute unit (0: all);
+// the rest is then a product of its own.
+int64_t whole_rows(int64_t M, int N) {
+  const int64_t nN = (N + kBM - 1) / kBM, nM = (M + kBM - 1) / kBM;
+  const int64_t whole = nM * nN / kCus * kCus / nN;
+  return whole > 0 && whole < nM ? whole * kBM : 0;
+}
+Plan plan_product(int64_t M, int N, int K, int most, bool direct) {
+  Plan best;
+  const double c = plan_small(M, N, K, most, direct, &best);
+  if (direct) {
+    const int64_t first = whole_rows(M, N);
+    Plan rest;
+    double d = plan_cost(M, N, K, {8, 1});
+    if (first > 0) d = std::min(d, plan_cost(first, N, K, {8, 1}) + plan_small(M - first, N, K, 1, true, &rest));
+    if (d < c) best = {8, 1};
   }
   return without_empty(best, K);
 }
-Plan plan_product(int64_t M, int N, int K, int most, bool direct) { return plan_any(M, N, K, most, 1, direct); }
 // A weight gradient over T tokens: of the eight-wave form as many token slices as
 // make two whole rounds.
 Plan plan_wgrad(int64_t T, int N, int K, bool direct) {
   const int Ti = (int)std::max<int64_t>(T, 1);
-  const int64_t tiles = (int64_t)((N + kBM - 1) / kBM) * ((K + kBM - 1) / kBM);
-  int64_t n = std::max<int64_t>(1, 2 * kCus / tiles);
-  n = std::min(n, std::max<int64_t>(1, T / (4 * kBK)));
-  return plan_any(N, K, Ti, kMaxSplit, (int)std::min<int64_t>(n, kMaxTokenSlices), direct);
+  Plan best;
+  const double c = plan_small(N, K, Ti, kMaxSplit, direct, &best);
+  if (direct) {
+    const int64_t tiles = (int64_t)((N + kBM - 1) / kBM) * ((K + kBM - 1) / kBM);
+    int64_t n = std::max<int64_t>(1, 2 * kCus / tiles);
+    n = std::min(n, std::max<int64_t>(1, T / (4 * kBK)));
+    const Plan p = {8, (int)std::min<int64_t>(n, kMaxTokenSlices)};
+    if (plan_cost(N, K, Ti, p) < c) best = p;
+  }
+  return without_empty(best, Ti);
 }
 
 template <typename T, typename TO, bool KROW, int NW, bool F32>
 hipError_t gemm_launch(GemmArgs g, int ns, hipStream_t st) {
   constexpr int BM = NW == 8 ? kBM : kBS;
-  // stages of A and B: 3 + 2 of 32 KB, 4 + 4 of 16 KB, or 2 + 2 of 16 KB
-  constexpr size_t lds = (NW == 8 ? 5 : NW == 4 ? 8 : 4) * (size_t)BM * kBK * 2;   // NW 2 and 0: 64 KB
+  // stages of A and B: 3 + 2 of 32 KB (160 KB), or 2 + 2 of 16 KB
+  constexpr size_t lds = (NW == 8 ? 5 : 4) * (size_t)BM * kBK * 2;
   const int64_t tiles = (g.M + BM - 1) / BM * ((g.N + BM - 1) / BM);
   g.kslice = slice_len(g.K, ns);
   g.work = (int)(tiles * ns);
-  // one workgroup a compute unit is resident with direct loads: they walk the work
-  const int grid = NW == 8 || NW == 4 ? std::min(g.work, kCus) : g.work;
+  // eight waves: the one workgroup that is resident on each compute unit walks the work
+  const int grid = NW == 8 ? std::min(g.work, kCus) : g.work;
   hipLaunchKernelGGL((lin_gemm_kernel<T, TO, KROW, NW, F32>), dim3(grid), dim3(NW == 8 ? 512 : 256), lds, st, g);
   return hipGetLastError();
 }
@@ -939,7 +965,6 @@ template <typename T, typename TO, bool KROW, bool F32>
 hipError_t gemm_planned(const GemmArgs& g, Plan p, hipStream_t st) {
   switch (p.nw) {
     case 8: return gemm_launch<T, TO, KROW, 8, F32>(g, p.ns, st);
-    case 4: return gemm_launch<T, TO, KROW, 4, F32>(g, p.ns, st);
     case 2: return gemm_launch<T, TO, KROW, 2, F32>(g, p.ns, st);
     default: return gemm_launch<T, TO, KROW, 0, F32>(g, p.ns, st);
   }
@@ -980,15 +1005,15 @@ hipError_t row_product(GemmArgs g, float* part, hipStream_t st) {
   const bool direct = direct_ok(g.a, g.lda, kBM) && direct_ok(g.b, g.ldb, kBM) && g.row_bytes % 16 == 0;
   Plan p = plan_product(g.M, g.N, g.K, kMaxSplit, direct);
   if (p.nw == 8) {
-    const int64_t nN = (g.N + kBM - 1) / kBM, nM = (g.M + kBM - 1) / kBM;
-    const int64_t whole = nM * nN / kCus * kCus / nN;       // row tiles in whole rounds
-    if (whole > 0 && whole < nM) {
+    const int64_t rows = whole_rows(g.M, g.N);
+    Plan rest;
+    if (rows > 0 && plan_cost(rows, g.N, g.K, {8, 1}) + plan_small(g.M - rows, g.N, g.K, 1, true, &rest) < plan_cost(g.M, g.N, g.K, {8, 1})) {
       GemmArgs first = g;
-      first.M = whole * kBM;
+      first.M = rows;
       const hipError_t e = product_form<T, TO, true>(first, Plan{8, 1}, false, nullptr, st);
       if (e != hipSuccess) return e;
       skip_rows<TO>(g, first.M);
-      p = plan_product(g.M, g.N, g.K, 1, true);             // no slices: `part` may not hold them
+      p = rest;                                             // in one slice: `part` may not hold more
     }
   }
   return product_form<T, TO, true>(g, p, false, part, st);
@@ -1007,6 +1032,11 @@ hipError_t skinny_rt(const SkinnyArgs& g, hipStream_t st) {
   if (rt == 2) hipLaunchKernelGGL((skinny_kernel<T, TO, MT, 2>), grid, dim3(64 * waves), lds, st, g);
   else hipLaunchKernelGGL((skinny_kernel<T, TO, MT, 1>), grid, dim3(64 * waves), lds, st, g);
   return hipGetLastError();
+}
+
+template <typename T, typename TO>
+hipError_t skinny(const SkinnyArgs& g, hipStream_t st) {
+  return g.M <= 16 ? skinny_rt<T, TO, 1>(g, st) : g.M <= 32 ? skinny_rt<T, TO, 2>(g, st) : skinny_rt<T, TO, 4>(g, st);
 }
 
 size_t split_floats(int64_t M, int N, int K, bool direct) {
@@ -1046,7 +1076,7 @@ hipError_t fwd_t(const LinFwd& a, void* ws, hipStream_t st) {
   e.y_ld = a.y_ld; e.pre_ld = a.pre_ld; e.res_ld = a.res_ld; e.act = a.act;
   if (a.M <= kSkinnyMost) {
     SkinnyArgs g = {(const char*)a.x, (const char*)a.w, a.x_ld * ES, a.w_ld * ES, (int)a.M, a.N, a.K * ES, e};
-    return a.M <= 16 ? skinny_rt<T, TO, 1>(g, st) : a.M <= 32 ? skinny_rt<T, TO, 2>(g, st) : skinny_rt<T, TO, 4>(g, st);
+    return skinny<T, TO>(g, st);
   }
   GemmArgs g = {};
   g.a = (const char*)a.x; g.b = (const char*)a.w; g.lda = a.x_ld * ES; g.ldb = a.w_ld * ES;
@@ -1122,7 +1152,13 @@ hipError_t bwd_t(const LinBwd& a, char* ws, hipStream_t st) {
     g.a = d; g.lda = d_ld; g.b = (const char*)wt; g.ldb = 2 * w.dt_ld;
     g.M = a.M; g.N = a.K; g.K = (int)w.dt_ld; g.row_bytes = 2 * (int)w.dt_ld;
     g.e.y = a.dx; g.e.y_ld = a.dx_ld;
-    if ((e = row_product<T, T>(g, part, st)) != hipSuccess) return e;
+    if (a.M <= kSkinnyMost) {
+      const SkinnyArgs k = {g.a, g.b, g.lda, g.ldb, (int)a.M, a.K, g.row_bytes, g.e};
+      e = skinny<T, T>(k, st);
+    } else {
+      e = row_product<T, T>(g, part, st);
+    }
+    if (e != hipSuccess) return e;
   }
   if (a.dw != nullptr) {
     GemmArgs g = {};
