@@ -314,6 +314,12 @@ int terra_internal_product_plan(int M, int N, int K, int max_split) {
   return terra::block_product_plan(M, N, K, max_split);
 }
 int terra_internal_wgrad_plan(int T, int Nl, int Kl) { return terra::block_wgrad_plan(T, Nl, Kl); }
+int terra_internal_linear_form(int64_t M, int N, int K, int dtype, int aligned) {
+  return terra::lin_form(M, N, K, dtype, aligned != 0);
+}
+int terra_internal_linear_wgrad_form(int64_t M, int N, int K, int aligned) {
+  return terra::lin_wgrad_form(M, N, K, aligned != 0);
+}
 int terra_internal_attn_waves(const terra_geom* g, int dtype, int which) {
   const int s = check_attn(g, dtype);
   return s ? -s : terra::attn_waves(launch_geo(g), dtype, which);

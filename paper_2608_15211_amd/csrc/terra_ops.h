@@ -85,6 +85,8 @@ struct LinBwd {
   bool dw_f32;
 };
 
+int lin_form(int64_t M, int N, int K, int dtype, bool aligned);
+int lin_wgrad_form(int64_t M, int N, int K, bool aligned);
 size_t lin_fwd_workspace(int64_t M, int N, int K, int dtype);
 size_t lin_bwd_workspace(int64_t M, int N, int K);
 hipError_t launch_lin_fwd(int dtype, int out, const LinFwd& a, void* ws, hipStream_t st);

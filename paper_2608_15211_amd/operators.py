@@ -252,17 +252,19 @@ def terra_linear_bwd_workspace_bytes(M, N, K, dtype):
 
 
 def terra_linear_fwd(x, w, bias=None, act="none", res=None, x_scale=None, w_scale=None, out=None, pre=None,
-                     workspace=None, out_dtype=torch.bfloat16):
+                     workspace=None, out_dtype=None):
     """y = act(x w^T + bias) + res for x (..., K) and w (N, K), act one of
     none, relu, gelu, silu.  bfloat16 or float16 tensors, or float8_e4m3fn x
     and w with x_scale (float32, one a row of x) and w_scale (N), y then of
-    out_dtype.  pre (like y) receives what act is applied to, for the backward."""
+    out_dtype (default bfloat16).  pre (like y) receives what act is applied to, for the backward."""
     dev, dt = _input(x, "x"), x.dtype
     if w.dim() != 2:
         raise ValueError("w must have two dimensions")
     (N, K), code = w.shape, _code(dt)
     M = x.numel() // K if K else 0
-    to = out_dtype if code == TERRA_E4M3 else dt
+    to = dt if code != TERRA_E4M3 else out_dtype or torch.bfloat16
+    if out_dtype not in (None, to):
+        raise ValueError("out_dtype is %s for %s tensors" % (to, dt))
     if out is None:
         out = torch.empty((*x.shape[:-1], N), dtype=to, device=x.device)
     (xp, xl), (wp, wl) = _matrix(x, "x", dev, dt, M, K), _matrix(w, "w", dev, dt, N, K)

@@ -49,7 +49,9 @@ def check(y, pre, x, w, bias, act, res, sx=None, sw=None):
 # do not take
 SIZES = [(1, 1, 1), (1, 16, 64), (1, 77, 130), (1, 4096, 768), (3, 33, 1000), (16, 100, 256), (17, 48, 72), (33, 130, 515),
          (48, 300, 64), (64, 65, 1024), (65, 64, 64), (100, 129, 40), (128, 128, 512), (130, 1000, 2048), (200, 257, 1111),
-         (513, 8, 4096), (300, 2305, 96), (1017, 771, 1003), (2500, 2000, 264), (4000, 4200, 128)]
+         (513, 8, 4096), (300, 2305, 96), (1017, 771, 1003), (2500, 2000, 264), (4000, 4200, 128),
+         (5, 16400, 72), (20, 16390, 64), (40, 16500, 136), (2000, 2000, 2003), (6000, 2100, 1003),
+         (5000, 4100, 1024)]
 
 
 @pytest.mark.parametrize("dtype", [BF16, F16, E4M3])

@@ -194,7 +194,11 @@ def test_captured_and_replayed():
 
 
 def test_another_stream():
+    from paper_2608_15211_amd import operators as ops
     p = params(BF16)
+    for s in (torch.cuda.current_stream(), torch.cuda.Stream()):
+        with torch.cuda.stream(s):
+            assert ops._raw_stream(0) == torch.cuda.current_stream().cuda_stream and ops._current_device() == torch.cuda.current_device()
     first, blk = Block(p), Block({n: v.clone() for n, v in p.items()})
     first.step()
     torch.cuda.synchronize()

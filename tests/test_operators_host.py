@@ -117,6 +117,29 @@ def test_linear_workspaces():
         assert 0 < b(M, 768, 768, "bf16") < 3 * (M + 768) * 768 * 2 + 64 * 768 * 768 * 4 + 512 * 768 * 4 + (1 << 20)
 
 
+def test_linear_cases_reach_every_form():
+    """The GPU tests' sizes run each of the library's forms (256 compute units)."""
+    import test_gpu_linear as cases
+    L = P.lib()
+    L.terra_internal_linear_form.argtypes = [ctypes.c_int64, ctypes.c_int, ctypes.c_int, ctypes.c_int, ctypes.c_int]
+    L.terra_internal_linear_wgrad_form.argtypes = [ctypes.c_int64, ctypes.c_int, ctypes.c_int, ctypes.c_int]
+    few, forms, wgrad = set(), set(), set()
+    for M, N, K in cases.SIZES + [(256 * 43 + 19, 1536, 64)]:
+        for dtype in (BF16, E4M3):
+            f = L.terra_internal_linear_form(M, N, K, dtype, 1)
+            (few if M <= 64 else forms).add(f if M <= 64 else (f // 10000, f // 1000 % 10, f // 100 % 10, min(2, f % 100)))
+    for M, N, K in cases.BWD:
+        f = L.terra_internal_linear_wgrad_form(M, N, K, 1)
+        wgrad.add((f // 100, min(2, f % 100)))
+    assert few == {1, 2, 4, 11, 12, 14}
+    # (whole rounds and a rest, padded, form, in slices)
+    assert {f[1:] for f in forms} >= {(0, 8, 1), (0, 2, 1), (0, 2, 2), (0, 0, 1), (0, 0, 2), (1, 8, 1), (1, 2, 1)}
+    assert any(f[0] for f in forms)
+    assert wgrad >= {(2, 1), (2, 2), (8, 2)}
+    # rows at odd places
+    assert L.terra_internal_linear_form(333, 130, 70, BF16, 0) // 100 == 0
+
+
 # --------------------------------------------------------------------- rope
 def rope_desc(**kw):
     d = dict(head_dim=64, rot_dim=64, axes=1, layout=1, scaling=0, base=1e4, factor=1.0, orig_len=0.0, beta_fast=32.0, beta_slow=1.0,
@@ -194,6 +217,30 @@ def test_binding_refuses_host_tensors_and_names():
         P.terra_plan_rope(64, scaling="more")
     with pytest.raises(P.TerraError):
         P.terra_plan_rope(64, rot_dim=65)
+
+
+def test_calls_go_to_the_tensors_device(monkeypatch):
+    """On another device than the current one: there, on its stream; back afterwards."""
+    o, at = ops(), [0]
+
+    class Device:
+        def __init__(self, i):
+            self.i = i
+
+        def __enter__(self):
+            self.was, at[0] = at[0], self.i
+
+        def __exit__(self, *a):
+            at[0] = self.was
+
+    monkeypatch.setattr(torch.cuda, "device", Device)
+    monkeypatch.setattr(o, "_current_device", lambda: at[0])
+    monkeypatch.setattr(o, "_raw_stream", lambda i: 100 + i)
+    seen = []
+    call = lambda *a: seen.append((at[0], a)) or 0  # noqa: E731
+    o._call(call, 0, "x")
+    o._call(call, 3, "y")
+    assert seen == [(0, ("x", 100)), (3, ("y", 103))] and at[0] == 0
 
 
 def test_row_strides():
