@@ -87,14 +87,25 @@ __global__ __launch_bounds__(kRopeThreads) void rope_kernel(RopeArgs a) {
       const T* in = (const T*)s.in + (tok0 + t) * s.in_t + head * s.in_h;
       T* out = (T*)s.out + (tok0 + t) * s.out_t + head * s.out_h;
       if (u < a.turned) {
-        const int p = u * V;
-        const float2* cs = angles + t * a.pairs + p;
-        if (HALF) {
-          const int lo = p + (p >= a.half ? a.half : 0);     // channel of the first of each pair
+        // pairs [i, i + V) of an axis, as many as there are
+        const int axis = u >= a.upa ? 1 : 0;
+        const int i = (u - axis * a.upa) * V, left = a.half - i;
+        const float2* cs = angles + t * a.pairs + axis * a.half + i;
+        // channels of the first pair
+        const int lo = 2 * axis * a.half + (HALF ? i : 2 * i);
+        if (left < V) {
+          for (int x = 0; x < left; ++x) {
+            const int c0 = HALF ? lo + x : lo + 2 * x, c1 = HALF ? c0 + a.half : c0 + 1;
+            const float2 c = cs[x];
+            const float xf = to_float<T>(in[c0]), yf = to_float<T>(in[c1]);
+            out[c0] = from_float<T>(fmaf(xf, c.x, -yf * c.y));
+            out[c1] = from_float<T>(fmaf(xf, c.y, yf * c.x));
+          }
+        } else if (HALF) {
           Vec<T, V> x, y;
           __builtin_memcpy(&x, in + lo, sizeof(x));
           __builtin_memcpy(&y, in + lo + a.half, sizeof(y));
-  #pragma unroll
+#pragma unroll
           for (int i = 0; i < V; ++i) {
             const float2 c = cs[i];
             const float xf = to_float<T>(x.v[i]), yf = to_float<T>(y.v[i]);
@@ -105,22 +116,24 @@ __global__ __launch_bounds__(kRopeThreads) void rope_kernel(RopeArgs a) {
           __builtin_memcpy(out + lo + a.half, &y, sizeof(y));
         } else {
           Vec<T, 2 * V> x;
-          __builtin_memcpy(&x, in + 2 * p, sizeof(x));
-  #pragma unroll
+          __builtin_memcpy(&x, in + lo, sizeof(x));
+#pragma unroll
           for (int i = 0; i < V; ++i) {
             const float2 c = cs[i];
             const float xf = to_float<T>(x.v[2 * i]), yf = to_float<T>(x.v[2 * i + 1]);
             x.v[2 * i] = from_float<T>(fmaf(xf, c.x, -yf * c.y));
             x.v[2 * i + 1] = from_float<T>(fmaf(xf, c.y, yf * c.x));
           }
-          __builtin_memcpy(out + 2 * p, &x, sizeof(x));
+          __builtin_memcpy(out + lo, &x, sizeof(x));
         }
       } else {
+        // copied channels; the last unit ends with the head and may repeat some
         const int c0 = 2 * a.pairs + (u - a.turned) * 2 * V;
-        if (c0 + 2 * V <= a.hd) {
+        if (a.hd - 2 * a.pairs >= 2 * V) {
+          const int c = min(c0, a.hd - 2 * V);
           Vec<T, 2 * V> x;
-          __builtin_memcpy(&x, in + c0, sizeof(x));
-          __builtin_memcpy(out + c0, &x, sizeof(x));
+          __builtin_memcpy(&x, in + c, sizeof(x));
+          __builtin_memcpy(out + c, &x, sizeof(x));
         } else {
           for (int c = c0; c < a.hd; ++c) out[c] = in[c];
         }
@@ -167,19 +180,24 @@ void rope_turns(double base, int scaling, double factor, double orig_len, double
 
 hipError_t launch_rope(int dtype, RopeArgs a, bool half, hipStream_t st) {
   if (a.tokens == 0) return hipSuccess;
-  // the most pairs a unit: 8 (16-byte accesses of 16-bit types), fewer where
-  // they do not divide an axis's pairs
+  // pairs a unit: 8 (16-byte accesses of 16-bit types), fewer where an axis has
+  // fewer or half as many leave none over; what is left goes pair by pair (26 pairs
+  // of 24 heads: 13.9 us against 15.8 in units of two; 6 pairs: 11.8 in units of
+  // four, 9 in units of two)
   int v = 8;
-  while (a.half % v != 0) v /= 2;
-  const bool copy = a.hd > 2 * a.pairs && !(a.side[0].in == a.side[0].out && (a.side[1].heads == 0 || a.side[1].in == a.side[1].out));
-  a.turned = a.pairs / v;
+  while (v > a.half || (v > 2 && a.half % v != 0 && a.half % (v / 2) == 0)) v /= 2;
+  const bool in_place = a.side[0].in == a.side[0].out && (a.side[1].heads == 0 || a.side[1].in == a.side[1].out);
+  const bool copy = a.hd > 2 * a.pairs && !in_place;
+  a.upa = (a.half + v - 1) / v;
+  a.turned = a.axes * a.upa;
   a.uph = a.turned + (copy ? (a.hd - 2 * a.pairs + 2 * v - 1) / (2 * v) : 0);
   a.units = a.uph * (a.side[0].heads + a.side[1].heads);
-  // tokens a workgroup: about six units a thread, while the angles fit, and
-  // fewer where that would leave compute units idle
-  int64_t tb = (6 * kRopeThreads + a.units - 1) / a.units;
+  // tokens a workgroup: about two units a thread (138240 tokens of 2 x 24 heads of
+  // 32, bf16: 164 us, with six 178; 31401 of 15 heads of 64 29.6 and 32.7), while
+  // the angles fit, and fewer where that would leave compute units idle
+  int64_t tb = (2 * kRopeThreads + a.units - 1) / a.units;
   tb = std::min<int64_t>(tb, std::max(1, kRopeAngles / a.pairs));
-  tb = std::min<int64_t>(tb, std::max<int64_t>(1, a.tokens / 512));
+  tb = std::min<int64_t>(tb, std::max<int64_t>(1, a.tokens / 1024));
   a.tb = (int)tb;
   a.rpairs = 1.0f / (float)a.pairs;
   a.runits = 1.0f / (float)a.units;

@@ -52,8 +52,8 @@ struct RopeArgs {
   uint32_t grid_w, grid_hw;
   float scale, sin_scale;  // factors on cosine and sine
   // set by launch_rope: tokens a workgroup, units of a token and of a head,
-  // how many of these turn, and the reciprocals fast_div starts from
-  int tb, units, uph, turned;
+  // how many of these turn, of an axis, and the reciprocals fast_div starts from
+  int tb, units, uph, turned, upa;
   float rpairs, runits, ruph;
   uint64_t turns[kRopePairs];
 };
