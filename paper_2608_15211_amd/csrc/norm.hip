@@ -484,15 +484,17 @@ hipError_t launch_rms_fwd(int dtype, const RmsFwd& a, hipStream_t st) {
   return dtype == 0 ? fwd_t<float>(a, st) : dtype == 1 ? fwd_t<__bf16>(a, st) : fwd_t<_Float16>(a, st);
 }
 
-hipError_t launch_rms_bwd(int dtype, const RmsBwd& a, float* dgain, hipStream_t st) {
+hipError_t launch_rms_bwd(int dtype, RmsBwd a, float* dgain, hipStream_t st) {
   const int blocks = rms_bwd_blocks(a.rows, a.cols);
+  const bool alone = dgain != nullptr && blocks == 1;      // one workgroup's sums are the sums
+  if (alone) a.part = dgain;
   if (blocks > 0 && (a.dx != nullptr || dgain != nullptr)) {
     const hipError_t e = dtype == 0   ? bwd_t<float>(a, blocks, st)
                          : dtype == 1 ? bwd_t<__bf16>(a, blocks, st)
                                       : bwd_t<_Float16>(a, blocks, st);
     if (e != hipSuccess) return e;
   }
-  return dgain == nullptr ? hipSuccess : launch_part_sum(a.part, dgain, blocks, a.cols, st);
+  return dgain == nullptr || alone ? hipSuccess : launch_part_sum(a.part, dgain, blocks, a.cols, st);
 }
 
 }  // namespace terra

@@ -32,7 +32,7 @@ hipError_t launch_part_sum(const float* part, float* out, int n, int cols, hipSt
 
 int rms_bwd_blocks(int64_t rows, int cols);
 hipError_t launch_rms_fwd(int dtype, const RmsFwd& a, hipStream_t st);
-hipError_t launch_rms_bwd(int dtype, const RmsBwd& a, float* dgain, hipStream_t st);
+hipError_t launch_rms_bwd(int dtype, RmsBwd a, float* dgain, hipStream_t st);
 
 constexpr int kRopePairs = 128;    // of one head, at most
 
