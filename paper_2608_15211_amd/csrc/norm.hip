@@ -405,8 +405,9 @@ __global__ __launch_bounds__(1024) void part_sum_kernel(const float* __restrict_
 // Threads a row and chunks a thread (one or two: with four the backward's
 // sums, the row and its successor no longer fit the registers).  One wave a row up
 // to 1024 columns, where rows are many: a row's sums then need no barrier.  Few
-// rows, and longer ones, take a workgroup each.  `most`: chunks a thread at
-// 1024 threads, which have 128 registers each.
+// rows, and longer ones, take a workgroup each (9479 rows of 6751 into e4m3: 512
+// threads 131 us, 1024 threads 167).  `most`: chunks a thread at 1024
+// threads, which have 128 registers each.
 struct RowForm {
   int tpr, nch;           // tpr 0: the long form
 };
@@ -415,7 +416,8 @@ RowForm row_form(int64_t rows, int cols, int most) {
   auto pick = [&](int tpr) { return RowForm{tpr, chunks <= tpr ? 1 : 2}; };
   if (chunks <= 64 || (chunks <= 128 && rows > 1024)) return pick(64);
   if (chunks <= 512) return pick(256);
-  if (chunks <= 1024 * most) return pick(1024);
+  if (chunks <= 1024) return RowForm{512, 2};
+  if (chunks <= 1024 * most) return RowForm{1024, 2};
   return RowForm{0, 0};
 }
 constexpr int kFwdMost = 2, kBwdMost = 1;
@@ -432,7 +434,7 @@ constexpr int kFwdMost = 2, kBwdMost = 1;
     case 66: TERRA_ROW_FORM(KERNEL, T, 64, 2, 256);             \
     case 257: TERRA_ROW_FORM(KERNEL, T, 256, 1, 256);           \
     case 258: TERRA_ROW_FORM(KERNEL, T, 256, 2, 256);           \
-    case 1025: TERRA_ROW_FORM(KERNEL, T, 1024, 1, 1024);
+    case 514: TERRA_ROW_FORM(KERNEL, T, 512, 2, 512);
 
 namespace {
 
@@ -442,7 +444,7 @@ int row_blocks(int64_t rows, int per, int64_t most) {
   return (int)(b < most ? b : most);
 }
 int row_blocks(int64_t rows, const RowForm& f, bool bwd) {
-  if (f.tpr == 0 || f.tpr == 1024) return row_blocks(rows, 1, 512);
+  if (f.tpr == 0 || f.tpr >= 512) return row_blocks(rows, 1, 512);
   return row_blocks(rows, f.tpr == 64 ? 4 : 1, 256 * (f.nch == 2 ? (bwd ? 3 : 5) : (bwd ? 5 : 8)));
 }
 
