@@ -615,7 +615,7 @@ static int check_rms(const terra_rmsnorm_desc* d, int dtype) {
   if (s) return s;
   if (d->rows < 0 || d->cols < 1) return fail(TERRA_ERR_INVALID, "rows must be >= 0 and cols >= 1");
   if (!(d->eps >= 0.0f && d->eps < INFINITY)) return fail(TERRA_ERR_INVALID, "eps must be finite and >= 0");
-  if (d->cols > (1 << 28)) return fail(TERRA_ERR_UNSUPPORTED, "cols must be at most 2^28");
+  if (d->cols > (1 << 24)) return fail(TERRA_ERR_UNSUPPORTED, "cols must be at most 2^24");
   return ok();
 }
 
@@ -693,8 +693,8 @@ int terra_rmsnorm_bwd(const terra_rmsnorm_desc* d, int dtype, const void* dy, co
 
 static int check_linear_size(int64_t M, int32_t N, int32_t K) {
   if (M < 0 || N < 1 || K < 1) return fail(TERRA_ERR_INVALID, "M must be >= 0, N and K >= 1");
-  if (M >= ((int64_t)1 << 31) - 256 || N > (1 << 28) || K > (1 << 28))
-    return fail(TERRA_ERR_UNSUPPORTED, "M must be below 2^31 - 256, N and K at most 2^28");
+  if (M >= ((int64_t)1 << 31) - 256 || N > (1 << 26) || K > (1 << 26))
+    return fail(TERRA_ERR_UNSUPPORTED, "M must be below 2^31 - 256, N and K at most 2^26");
   // a launch takes fewer than 2^32 threads: 64 x 64 tiles of 256 of them, at most
   auto tiles = [](int64_t a, int64_t b) { return ((a + 127) / 128) * ((b + 127) / 128); };
   if (tiles(M, N) >= (1 << 21) || tiles(M, K) >= (1 << 21) || tiles(N, K) >= (1 << 21))

@@ -38,7 +38,7 @@ def norm_fwd(dtype=BF16, x=A, res=None, gain=None, z=None, y=A, q=None, qs=None,
 
 @pytest.mark.parametrize("kw,want", [
     (dict(rows=0), OK), (dict(rows=0, x=None, y=None), OK), (dict(rows=-1), INVALID), (dict(cols=0), INVALID),
-    (dict(cols=(1 << 28) + 1, x_ld=1 << 30, y_ld=1 << 30), UNSUPPORTED), (dict(eps=-1.0), INVALID),
+    (dict(cols=(1 << 24) + 1, x_ld=1 << 30, y_ld=1 << 30), UNSUPPORTED), (dict(eps=-1.0), INVALID),
     (dict(eps=math.nan), INVALID), (dict(eps=math.inf), INVALID), (dict(dtype=E4M3), INVALID), (dict(dtype=7), INVALID),
     (dict(x=None), INVALID), (dict(y=None), INVALID), (dict(q=A), INVALID), (dict(qs=A), INVALID), (dict(x_ld=7), INVALID),
     (dict(y_ld=7), INVALID), (dict(res=A, res_ld=0), INVALID), (dict(z=A, z_ld=-8), INVALID), (dict(q=A, qs=A, q_ld=1), INVALID),
@@ -80,7 +80,7 @@ def lin_fwd(dtype=BF16, x=A, xs=None, w=A, wsc=None, bias=None, res=None, y=A, p
 
 @pytest.mark.parametrize("kw,want", [
     (dict(M=0), OK), (dict(M=0, x=None), OK), (dict(M=-1), INVALID), (dict(N=0), INVALID), (dict(K=0), INVALID),
-    (dict(M=1 << 31), UNSUPPORTED), (dict(N=(1 << 28) + 1), UNSUPPORTED), (dict(M=1 << 30, N=1 << 20, y_ld=1 << 20), UNSUPPORTED),
+    (dict(M=1 << 31), UNSUPPORTED), (dict(N=(1 << 26) + 1), UNSUPPORTED), (dict(K=(1 << 26) + 1), UNSUPPORTED), (dict(M=1 << 30, N=1 << 20, y_ld=1 << 20), UNSUPPORTED),
     (dict(act=4), INVALID), (dict(act=-1), INVALID), (dict(dtype=F32), UNSUPPORTED), (dict(dtype=9), INVALID),
     (dict(out_dtype=F32), INVALID), (dict(out_dtype=F16), INVALID), (dict(dtype=E4M3), INVALID),
     (dict(dtype=E4M3, xs=A), INVALID), (dict(dtype=E4M3, xs=A, wsc=A, out_dtype=E4M3), INVALID), (dict(xs=A), INVALID), (dict(wsc=A), INVALID),
