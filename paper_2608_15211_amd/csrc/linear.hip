@@ -674,7 +674,7 @@ __global__ __launch_bounds__(1024) void skinny_kernel(SkinnyArgs g) {
     for (int j = 0; j < RT; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
   const int full = g.row_bytes >> 7;
   // U pieces at a time, so that their loads go out together
-  constexpr int U = MT + RT <= 2 ? 4 : MT + RT <= 4 ? 2 : 1;
+  constexpr int U = MT + RT <= 3 ? 4 : MT + RT <= 5 ? 2 : 1;
   auto pieces = [&](int it, auto count) {
     constexpr int C = decltype(count)::value;
     i32x4 a[C][RT][2], b[C][MT][2];
@@ -870,8 +870,8 @@ int slice_len(int K, int ns) { return ((K + ns - 1) / ns + kBK - 1) / kBK * kBK;
 // The form of a product (nw: NW of lin_gemm_kernel) and its contraction slices,
 // by the time of the busiest compute unit, in us: a stage of 64 units takes 1.45
 // with eight waves; in form 2 0.65 for one workgroup on a unit and 1.05 for each
-// of two; through registers 1.7 (of two); a workgroup 9 with eight waves and 3
-// to 4 besides; a sum of slices 5 and its traffic.  Measured in one slice, eight
+// of two, through registers 1.7 and 3.0; a workgroup 9 with eight waves, 3 and 4, 5
+// and 10 besides; a sum of slices 5 and its traffic.  Measured in one slice, eight
 // waves and form 2 (bf16, M x N x K): 2048 x 2048 x 1024 28.2 and 17.3 us, 4096
 // x 2048 x 512 21.9 and 16.4, 1441 x 4928 x 1856 46.8 and 36.9, 4096 x 4096 x
 // 1024 36.2 and 42.3, 8192 x 2048 x 2048 59 and 72, 34560 x 1024 x 4096 295
@@ -882,11 +882,11 @@ struct Plan {
 double plan_cost(int64_t M, int N, int K, Plan p) {
   const int bm = p.nw == 8 ? kBM : kBS;
   const double work = (double)((M + bm - 1) / bm) * ((N + bm - 1) / bm) * p.ns;
-  const bool pairs = p.nw == 0 || (p.nw == 2 && work > kCus);      // two workgroups a unit at once
+  const bool pairs = p.nw != 8 && work > kCus;                      // two workgroups a unit at once
   const double rounds = (double)(int64_t)((work + (pairs ? 2 : 1) * kCus - 1) / ((pairs ? 2 : 1) * kCus));
   const int stages = slice_len(K, p.ns) / kBK;
   const double sum = p.ns > 1 ? 5.0 + 0.8e-6 * p.ns * M * N : 0.0;
-  const double each = p.nw == 8 ? 1.45 * stages + 9.0 : p.nw == 0 ? 1.7 * stages + 3.0 : pairs ? 1.05 * stages + 4.0 : 0.65 * stages + 3.0;
+  const double each = p.nw == 8 ? 1.45 * stages + 9.0 : p.nw == 0 ? (pairs ? 3.0 * stages + 10.0 : 1.7 * stages + 5.0) : pairs ? 1.05 * stages + 4.0 : 0.65 * stages + 3.0;
   return rounds * each + sum;
 }
 Plan without_empty(Plan p, int K) {          // slices past the contraction's end
