@@ -581,6 +581,7 @@ __global__ __launch_bounds__(256) void slices_kernel(const float* __restrict__ p
   const int64_t m = idx / chunks;
   const int n = 8 * (int)(idx - m * chunks);
   float v[8] = {};
+#pragma unroll 4
   for (int s = 0; s < ns; ++s) {
     float p[8];
     __builtin_memcpy(p, __builtin_assume_aligned(part + s * f_slice + m * f_ld + n, 16), sizeof(p));
@@ -1114,7 +1115,8 @@ struct BwdWs {
 BwdWs bwd_ws(int64_t M, int N, int K) {
   BwdWs w;
   w.dt_ld = up8(N);
-  w.runs = (int)std::min<int64_t>(kMaxRuns, std::max<int64_t>(1, (M + 63) / 64));
+  // one run up to 64 rows (its sums are dbias), else of 16 rows or more
+  w.runs = M <= 64 ? 1 : (int)std::min<int64_t>(kMaxRuns, (M + 15) / 16);
   w.run = (M + w.runs - 1) / w.runs;
   size_t part = 0;
   for (bool direct : {false, true}) {

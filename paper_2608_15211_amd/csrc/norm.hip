@@ -387,6 +387,14 @@ __global__ __launch_bounds__(1024) void part_sum_kernel(const float* __restrict_
   float x[4] = {};
   if (col < cols) {
     int k = r;
+    // sixteen loads go out together
+    for (; k + 480 < n; k += 512) {
+      float v[16];
+#pragma unroll
+      for (int u = 0; u < 16; ++u) v[u] = part[(int64_t)(k + 32 * u) * cols + col];
+#pragma unroll
+      for (int u = 0; u < 16; ++u) x[u & 3] += v[u];
+    }
     for (; k + 96 < n; k += 128)
 #pragma unroll
       for (int u = 0; u < 4; ++u) x[u] += part[(int64_t)(k + 32 * u) * cols + col];
