@@ -186,6 +186,7 @@ __device__ __forceinline__ void finish8(const LinEpi& e, const LinCols& c, float
   store8((TO*)e.y + m * e.y_ld + n, nv, v);
 }
 
+// The same, fetching the row's scale.
 template <typename TO>
 __device__ inline void finish_row8(const LinEpi& e, const LinCols& c, int64_t m, int n, int nv, float (&v)[8]) {
   finish8<TO>(e, c, e.x_scale != nullptr ? e.x_scale[m] : 1.0f, m, n, nv, v);
@@ -237,9 +238,11 @@ __device__ __forceinline__ void drain(const LinEpi& e, const float* et, float co
   else rows(std::false_type{});
 }
 
-// Tile w of an nM x nN grid of tiles, above 12 columns in panels of up to eight, rows in turn within one:
-// the 32 tiles that an XCD's compute units work on at a time are then about 4 x 8
-// and share most of what they read.
+// Tile w of an nM x nN grid of tiles, above 12 columns in panels of up to eight,
+// rows in turn within one: the 32 tiles that an XCD's compute units work on at a
+// time are then about 4 x 8 and share most of what they read (34560 x 6144 x 1536
+// in e4m3 368 us against 393 in one panel, 8192 x 8192 x 4096 421 against 440; nine
+// columns as five and four 560 against 545).
 __device__ inline void panel_place(int w, int nM, int nN, int& tm, int& tn) {
   const int panels = nN <= 12 ? 1 : (nN + 7) >> 3, width = (nN + panels - 1) / panels;
   const int p = w / (nM * width), c = min(width, nN - p * width);
@@ -369,7 +372,8 @@ __global__ __launch_bounds__(NW == 8 ? 512 : 256, 1) void lin_gemm_kernel(GemmAr
     }
   };
   auto epilogue = [&](const Place& p, auto loaded) {
-    float* et = reinterpret_cast<float*>(smem) + (NW == 8 ? (wave < 4 ? 2 : 4) * (TL::kElems / 2) + (wave & 3) * 2048 : wave * 2048);
+    float* et = reinterpret_cast<float*>(smem) +
+                (NW == 8 ? (wave < 4 ? 2 : 4) * (TL::kElems / 2) + (wave & 3) * 2048 : wave * 2048);
     auto put = [&](const f32x16 (&a)[2]) {
 #pragma unroll
       for (int j = 0; j < 2; ++j)
@@ -390,7 +394,8 @@ __global__ __launch_bounds__(NW == 8 ? 512 : 256, 1) void lin_gemm_kernel(GemmAr
         default: put(acc[MI - 1]);
       }
       __builtin_amdgcn_wave_barrier();
-      drain<TO, F32, 32>(g.e, et, col_bias, col_scale, kScaled ? row_scale[kRS == 2 ? i >> 1 : 0] : 0.0f, 32 * (i & 1), p.m0 + wm + 32 * i, g.M, p.n0 + wn, g.N, p.z);
+      drain<TO, F32, 32>(g.e, et, col_bias, col_scale, kScaled ? row_scale[kRS == 2 ? i >> 1 : 0] : 0.0f, 32 * (i & 1),
+                         p.m0 + wm + 32 * i, g.M, p.n0 + wn, g.N, p.z);
       __builtin_amdgcn_wave_barrier();
     }
   };
