@@ -373,8 +373,9 @@ int terra_fragment_unpack(const terra_geom* g, int dtype, int32_t ranks, int32_t
  * are row-major with a row stride in elements (at least the row length); rows
  * may have any length and start at any multiple of the element size.  Tensors
  * of 16-byte rows at 16-byte places are the fast case.  A norm's row has at
- * most 2^24 columns; N and K of a linear layer are at most 2^26, M below 2^31,
- * and each of M N, M K and N K below 2^35.  No rows or tokens is a
+ * most 2^24 columns; N and K of a linear layer are at most 2^26, and each of
+ * M N, M K and N K, the sizes rounded up to multiples of 128, is below 2^35
+ * (TERRA_ERR_UNSUPPORTED where they are not).  No rows or tokens is a
  * valid call that does nothing (gradients of parameters are then zero).  A
  * workspace starts at a multiple of 16 bytes, belongs to one call at a time
  * (two calls that may overlap, or two captured graphs, need one each), and

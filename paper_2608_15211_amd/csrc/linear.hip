@@ -892,7 +892,9 @@ double plan_cost(int64_t M, int N, int K, Plan p) {
   const double rounds = (double)(int64_t)((work + (pairs ? 2 : 1) * kCus - 1) / ((pairs ? 2 : 1) * kCus));
   const int stages = slice_len(K, p.ns) / kBK;
   const double sum = p.ns > 1 ? 5.0 + 0.8e-6 * p.ns * M * N : 0.0;
-  const double each = p.nw == 8 ? 1.45 * stages + 9.0 : p.nw == 0 ? (pairs ? 3.0 * stages + 10.0 : 1.7 * stages + 5.0) : pairs ? 1.05 * stages + 4.0 : 0.65 * stages + 3.0;
+  const double each = p.nw == 8   ? 1.45 * stages + 9.0
+                      : p.nw == 2 ? (pairs ? 1.05 * stages + 4.0 : 0.65 * stages + 3.0)
+                                  : (pairs ? 3.0 * stages + 10.0 : 1.7 * stages + 5.0);
   return rounds * each + sum;
 }
 Plan without_empty(Plan p, int K) {          // slices past the contraction's end
