@@ -212,6 +212,75 @@ def test_another_stream():
         assert torch.equal(blk.g[name], first.g[name]), name
 
 
+def test_two_at_once():
+    """Two steps on two streams, eager and as two graphs, each with its own workspace."""
+    p = [params(BF16), params(BF16, seed=9)]
+    want = [Block({n: v.clone() for n, v in q.items()}) for q in p]
+    for w in want:
+        w.step()
+    blks = [Block(q) for q in p]
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    torch.cuda.synchronize()
+
+    def same():
+        torch.cuda.synchronize()
+        for blk, w in zip(blks, want):
+            for mine, theirs in ((blk.b, w.b), (blk.g, w.g)):
+                for name in mine:
+                    assert torch.equal(mine[name], theirs[name]), name
+                    mine[name].zero_()
+        torch.cuda.synchronize()
+
+    for _ in range(2):
+        for blk, s in zip(blks, streams):
+            with torch.cuda.stream(s):
+                blk.step()
+        same()
+    graphs = [torch.cuda.CUDAGraph() for _ in blks]
+    for blk, graph in zip(blks, graphs):
+        with torch.cuda.graph(graph):
+            blk.step()
+    for _ in range(3):
+        for graph, s in zip(graphs, streams):
+            with torch.cuda.stream(s):
+                graph.replay()
+        same()
+
+
+# few tokens, both tile sizes in one and in several slices, whole rounds and a rest, padded copies, any alignment
+@pytest.mark.parametrize("M,N,K,dtype", [(7, 300, 520, F16), (130, 1000, 2048, BF16), (300, 2304, 96, F16), (1017, 771, 1003, BF16),
+                                         (2000, 2000, 2003, F16), (11000, 1536, 64, BF16), (20000, 64, 64, F16)])
+def test_linear_captured(M, N, K, dtype):
+    """Graphs whose outputs and workspaces were allocated while they were captured."""
+    g = torch.Generator(device="cuda").manual_seed(5)
+    x, w, dy = (torch.empty(*d, dtype=dtype, device="cuda") for d in ((M, K), (N, K), (M, N)))
+    bias = torch.randn(N, generator=g, device="cuda")
+
+    def step():
+        pre = torch.empty(M, N, dtype=dtype, device="cuda")
+        y = P.terra_linear_fwd(x, w, bias, act="silu", pre=pre)
+        return (y, pre, *P.terra_linear_bwd(dy, x, w, pre, act="silu"))
+
+    def fill():
+        for t in (x, w, dy):
+            t.copy_(torch.randn(t.shape, generator=g, device="cuda"))
+
+    fill()
+    step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        outs = step()
+    for _ in range(3):
+        fill()
+        graph.replay()
+        want = step()
+        torch.cuda.synchronize()
+        for a, b in zip(outs, want):
+            assert torch.equal(a, b)
+            a.zero_()
+
+
 @pytest.mark.parametrize("rows", [1, 16, 40, 333])
 def test_norm_into_8_bit_product(rows):
     """The norm's 8-bit output and scales are what the product takes."""
