@@ -49,6 +49,59 @@ struct Vec {
 constexpr int kRopeThreads = 256;
 constexpr int kRopeAngles = 4096;
 
+// V pairs from the first one's channels: in the half layout the second of a pair
+// is `half` channels on, in the interleaved one the next.
+template <typename T, int V, bool HALF>
+__device__ inline void turn_pairs(const T* in, T* out, int half, const float2* cs) {
+  T x[V], y[V], p[2 * V];
+  if constexpr (HALF) {
+    __builtin_memcpy(x, in, sizeof(x));
+    __builtin_memcpy(y, in + half, sizeof(y));
+  } else {
+    __builtin_memcpy(p, in, sizeof(p));
+  }
+#pragma unroll
+  for (int i = 0; i < V; ++i) {
+    const float2 c = cs[i];
+    const float xf = to_float<T>(HALF ? x[i] : p[2 * i]), yf = to_float<T>(HALF ? y[i] : p[2 * i + 1]);
+    const T u = from_float<T>(fmaf(xf, c.x, -yf * c.y)), v = from_float<T>(fmaf(xf, c.y, yf * c.x));
+    if constexpr (HALF) { x[i] = u; y[i] = v; }
+    else { p[2 * i] = u; p[2 * i + 1] = v; }
+  }
+  if constexpr (HALF) {
+    __builtin_memcpy(out, x, sizeof(x));
+    __builtin_memcpy(out + half, y, sizeof(y));
+  } else {
+    __builtin_memcpy(out, p, sizeof(p));
+  }
+}
+// Up to V pairs, `left` of them there: all at once, or by halves (138240 tokens of
+// 2 x 24 heads of 32, 13 pairs, bf16: 443 us, 370 interleaved; pair by pair 724 and 621).
+template <typename T, int V, bool HALF>
+__device__ inline void turn_some(const T* in, T* out, int half, const float2* cs, int left) {
+  if (left >= V) return turn_pairs<T, V, HALF>(in, out, half, cs);
+  if constexpr (V > 1) {
+    constexpr int W = V / 2, C = HALF ? W : 2 * W;
+    if (left >= W) {
+      turn_pairs<T, W, HALF>(in, out, half, cs);
+      in += C; out += C; cs += W; left -= W;
+    }
+    if (left > 0) turn_some<T, W, HALF>(in, out, half, cs, left);
+  }
+}
+// Fewer than 2 V channels copied, by halves.
+template <typename T, int V>
+__device__ inline void copy_some(const T* in, T* out, int left) {
+  if (left >= V) {
+    T x[V];
+    __builtin_memcpy(x, in, sizeof(x));
+    __builtin_memcpy(out, x, sizeof(x));
+    in += V; out += V; left -= V;
+  }
+  if constexpr (V > 1)
+    if (left > 0) copy_some<T, V / 2>(in, out, left);
+}
+
 template <typename T, int V, bool HALF>
 __global__ __launch_bounds__(kRopeThreads) void rope_kernel(RopeArgs a) {
   extern __shared__ float2 angles[];       // [tb][pairs]
@@ -93,39 +146,7 @@ __global__ __launch_bounds__(kRopeThreads) void rope_kernel(RopeArgs a) {
         const float2* cs = angles + t * a.pairs + axis * a.half + i;
         // channels of the first pair
         const int lo = 2 * axis * a.half + (HALF ? i : 2 * i);
-        if (left < V) {
-          for (int x = 0; x < left; ++x) {
-            const int c0 = HALF ? lo + x : lo + 2 * x, c1 = HALF ? c0 + a.half : c0 + 1;
-            const float2 c = cs[x];
-            const float xf = to_float<T>(in[c0]), yf = to_float<T>(in[c1]);
-            out[c0] = from_float<T>(fmaf(xf, c.x, -yf * c.y));
-            out[c1] = from_float<T>(fmaf(xf, c.y, yf * c.x));
-          }
-        } else if (HALF) {
-          Vec<T, V> x, y;
-          __builtin_memcpy(&x, in + lo, sizeof(x));
-          __builtin_memcpy(&y, in + lo + a.half, sizeof(y));
-#pragma unroll
-          for (int i = 0; i < V; ++i) {
-            const float2 c = cs[i];
-            const float xf = to_float<T>(x.v[i]), yf = to_float<T>(y.v[i]);
-            x.v[i] = from_float<T>(fmaf(xf, c.x, -yf * c.y));
-            y.v[i] = from_float<T>(fmaf(xf, c.y, yf * c.x));
-          }
-          __builtin_memcpy(out + lo, &x, sizeof(x));
-          __builtin_memcpy(out + lo + a.half, &y, sizeof(y));
-        } else {
-          Vec<T, 2 * V> x;
-          __builtin_memcpy(&x, in + lo, sizeof(x));
-#pragma unroll
-          for (int i = 0; i < V; ++i) {
-            const float2 c = cs[i];
-            const float xf = to_float<T>(x.v[2 * i]), yf = to_float<T>(x.v[2 * i + 1]);
-            x.v[2 * i] = from_float<T>(fmaf(xf, c.x, -yf * c.y));
-            x.v[2 * i + 1] = from_float<T>(fmaf(xf, c.y, yf * c.x));
-          }
-          __builtin_memcpy(out + lo, &x, sizeof(x));
-        }
+        turn_some<T, V, HALF>(in + lo, out + lo, a.half, cs, left);
       } else {
         // copied channels; the last unit ends with the head and may repeat some
         const int c0 = 2 * a.pairs + (u - a.turned) * 2 * V;
@@ -135,7 +156,7 @@ __global__ __launch_bounds__(kRopeThreads) void rope_kernel(RopeArgs a) {
           __builtin_memcpy(&x, in + c, sizeof(x));
           __builtin_memcpy(out + c, &x, sizeof(x));
         } else {
-          for (int c = c0; c < a.hd; ++c) out[c] = in[c];
+          copy_some<T, V>(in + c0, out + c0, a.hd - c0);
         }
       }
     }
@@ -181,7 +202,7 @@ void rope_turns(double base, int scaling, double factor, double orig_len, double
 hipError_t launch_rope(int dtype, RopeArgs a, bool half, hipStream_t st) {
   if (a.tokens == 0) return hipSuccess;
   // pairs a unit: 8 (16-byte accesses of 16-bit types), fewer where an axis has
-  // fewer or half as many leave none over; what is left goes pair by pair (26 pairs
+  // fewer or half as many leave none over; what is left goes by fours, twos and ones (26 pairs
   // of 24 heads: 13.9 us against 15.8 in units of two; 6 pairs: 11.8 in units of
   // four, 9 in units of two)
   int v = 8;
