@@ -399,7 +399,8 @@ typedef struct terra_rmsnorm_desc {
  * `dtype` (TERRA_F32, TERRA_BF16, TERRA_F16); gain float32 (nullable: ones).
  * Outputs, each nullable, one at least: z and y of `dtype`, rstd float32 (for
  * the backward), and q (TERRA_E4M3) with q_scale (float32, one a row):
- *   q_scale = max(max |y| / 448, 2^-126),  q = y / q_scale to nearest even,
+ *   q_scale = max(max |y| / 448, 2^-126),  q = y / q_scale (the float32
+ *   quotient) to nearest even,
  * so that q * q_scale stands for y.  A NaN in a row makes its scale and the
  * row's y NaN.  z may be x or res, and y may be x, in place with the same
  * stride (not both the same). */

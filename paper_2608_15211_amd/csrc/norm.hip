@@ -70,6 +70,33 @@ __device__ inline float e4m3_scale(uint32_t amax) {
   return s < 1.17549435e-38f ? 1.17549435e-38f : s;
 }
 
+// The y of a row divided by its scale, |y / s| <= 448 but for rounding: the
+// float32 quotient, correctly rounded (a zero's sign aside), by its residuals.  With i = 1 / s
+// correctly rounded, q = y i is within 1.5 steps of it, q + (y - q s) i is one of
+// its two neighbours, and the same once more has an exact residual and rounds
+// correctly.  A power of two keeps the residuals of extreme scales normal (where they are not,
+// q is far below e4m3's smallest).  An infinite scale leaves 0 of finite y.  15301
+// x 1001 in bf16: 27.5 us; y i alone, a step of e4m3 off next to a tie, 26.6; the
+// division operator 29.6.
+struct E4m3Quotient {
+  float k, s, inv;
+  __device__ explicit E4m3Quotient(float scale) {
+    k = scale > 0x1p60f ? 0x1p-70f : scale < 0x1p-60f ? 0x1p70f : 1.0f;
+    s = scale * k;
+    inv = 1.0f / s;
+    if (inv == 0.0f) s = 0.0f;
+  }
+  __device__ void divide(float (&y)[8]) const {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float v = y[i] * k;
+      float q = v * inv;
+      q = fmaf(fmaf(-q, s, v), inv, q);
+      y[i] = fmaf(fmaf(-q, s, v), inv, q);
+    }
+  }
+};
+
 template <int TPR>
 struct Rows {
   static constexpr int kThreads = TPR == 64 ? 256 : TPR;
@@ -156,12 +183,11 @@ __global__ __launch_bounds__(Rows<TPR>::kThreads) void rms_fwd_kernel(RmsFwd a) 
         for (int i = 0; i < 8; ++i) amax = max(amax, mag(z[c][i]));
       const float s = e4m3_scale(row_max<TPR>(amax, red));
       if (t == 0) a.q_scale[row] = s;
-      const float inv = 1.0f / s;
+      const E4m3Quotient by(s);
 #pragma unroll
       for (int c = 0; c < NCH; ++c) {
         const int col = 8 * (t + TPR * c);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) z[c][i] *= inv;
+        by.divide(z[c]);
         store8_e4m3(a.q + row * a.q_ld + col, a.cols - col, z[c]);
       }
     }
@@ -202,14 +228,14 @@ __global__ __launch_bounds__(1024) void rms_fwd_long_kernel(RmsFwd a) {
       }
     }
     const float rstd = 1.0f / sqrtf(row_sum<1024>(ss, red) / (float)a.cols + a.eps);
-    float inv = 0.0f;
+    float s = 1.0f;
     if (a.q != nullptr) {
       const float m = __uint_as_float(row_max<1024>(amax, red)) * rstd;
-      const float s = e4m3_scale(mag(m));
-      inv = 1.0f / s;
+      s = e4m3_scale(mag(m));
       if (threadIdx.x == 0) a.q_scale[row] = s;
     }
     if (a.rstd != nullptr && threadIdx.x == 0) a.rstd[row] = rstd;
+    const E4m3Quotient by(s);
     for (int col = 8 * threadIdx.x; col < a.cols; col += 8192) {
       float z[8], g[8];
       load(row, col, z, g);
@@ -218,8 +244,7 @@ __global__ __launch_bounds__(1024) void rms_fwd_long_kernel(RmsFwd a) {
       for (int i = 0; i < 8; ++i) z[i] = z[i] * rstd * g[i];
       if (Y != nullptr) store8(Y + row * a.y_ld + col, a.cols - col, z);
       if (a.q != nullptr) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) z[i] *= inv;
+        by.divide(z);
         store8_e4m3(a.q + row * a.q_ld + col, a.cols - col, z);
       }
     }
