@@ -194,9 +194,11 @@ __global__ __launch_bounds__(Rows<TPR>::kThreads) void rms_fwd_kernel(RmsFwd a) 
   }
 }
 
-// Rows longer than the registers of a workgroup: read twice, the second time
-// from the L2.  Only the second pass writes, so that outputs in place of an
-// input are not read again.
+// Rows longer than the registers of a workgroup: read for the sum, once more for
+// the scale of an 8-bit output and for the outputs, after the first time from the
+// L2.  The scale is that of y itself: max |z gain| rstd, which the first pass could
+// find, overflows where y does not (1100 x 40000 in bf16: 198 us, with that 151).
+// Only the last pass writes, so that outputs in place of an input are not read again.
 template <typename T>
 __global__ __launch_bounds__(1024) void rms_fwd_long_kernel(RmsFwd a) {
   __shared__ float red[16];
@@ -204,44 +206,50 @@ __global__ __launch_bounds__(1024) void rms_fwd_long_kernel(RmsFwd a) {
   const T* R = (const T*)a.res;
   T* Z = (T*)a.z;
   T* Y = (T*)a.y;
-  auto load = [&](int64_t row, int col, float (&z)[8], float (&g)[8]) {
+  auto load_z = [&](int64_t row, int col, float (&z)[8]) {
     load8(X + row * a.x_ld + col, a.cols - col, z);
     if (R != nullptr) {
-      load8(R + row * a.res_ld + col, a.cols - col, g);
+      float r[8];
+      load8(R + row * a.res_ld + col, a.cols - col, r);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) z[i] += g[i];
+      for (int i = 0; i < 8; ++i) z[i] += r[i];
     }
-#pragma unroll
-    for (int i = 0; i < 8; ++i) g[i] = 1.0f;
+  };
+  auto times_gain = [&](int col, float rstd, float (&z)[8]) {
+    float g[8] = {1.0f, 1.0f, 1.0f, 1.0f, 1.0f, 1.0f, 1.0f, 1.0f};
     if (a.gain != nullptr) load8(a.gain + col, a.cols - col, g);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) z[i] = z[i] * rstd * g[i];
   };
   for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
     float ss = 0.0f;
-    uint32_t amax = 0;
     for (int col = 8 * threadIdx.x; col < a.cols; col += 8192) {
-      float z[8], g[8];
-      load(row, col, z, g);
+      float z[8];
+      load_z(row, col, z);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        ss = fmaf(z[i], z[i], ss);
-        amax = max(amax, mag(z[i] * g[i]));
-      }
+      for (int i = 0; i < 8; ++i) ss = fmaf(z[i], z[i], ss);
     }
     const float rstd = 1.0f / sqrtf(row_sum<1024>(ss, red) / (float)a.cols + a.eps);
     float s = 1.0f;
     if (a.q != nullptr) {
-      const float m = __uint_as_float(row_max<1024>(amax, red)) * rstd;
-      s = e4m3_scale(mag(m));
+      uint32_t amax = 0;
+      for (int col = 8 * threadIdx.x; col < a.cols; col += 8192) {
+        float y[8];
+        load_z(row, col, y);
+        times_gain(col, rstd, y);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) amax = max(amax, mag(y[i]));
+      }
+      s = e4m3_scale(row_max<1024>(amax, red));
       if (threadIdx.x == 0) a.q_scale[row] = s;
     }
     if (a.rstd != nullptr && threadIdx.x == 0) a.rstd[row] = rstd;
     const E4m3Quotient by(s);
     for (int col = 8 * threadIdx.x; col < a.cols; col += 8192) {
-      float z[8], g[8];
-      load(row, col, z, g);
+      float z[8];
+      load_z(row, col, z);
       if (Z != nullptr) store8(Z + row * a.z_ld + col, a.cols - col, z);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) z[i] = z[i] * rstd * g[i];
+      times_gain(col, rstd, z);
       if (Y != nullptr) store8(Y + row * a.y_ld + col, a.cols - col, z);
       if (a.q != nullptr) {
         by.divide(z);

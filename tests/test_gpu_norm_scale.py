@@ -1,5 +1,5 @@
-"""The 8-bit output of the root-mean-square norm: q is the nearest e4m3 value to the
-float32 quotient y / q_scale, bit for bit."""
+"""The 8-bit output of the root-mean-square norm: its scale is that of the row's y,
+and q the nearest e4m3 value to the float32 quotient y / q_scale, for every way a row is held."""
 
 import pytest
 
@@ -8,8 +8,8 @@ P = pytest.importorskip("paper_2608_15211_amd")
 
 pytestmark = pytest.mark.gpu
 F32, E4M3 = torch.float32, torch.float8_e4m3fn
-# (rows, cols): one wave, 256, 512 and 1024 threads a row; whole chunks and not
-SIZES = [(1030, 64), (1030, 509), (40, 1001), (40, 4096), (30, 8191), (20, 16384)]
+# (rows, cols): one wave, 256, 512 and 1024 threads a row, and rows that are read again; whole chunks and not
+SIZES = [(1030, 64), (1030, 509), (40, 1001), (40, 4096), (30, 8191), (20, 16384), (6, 16391), (5, 40003)]
 
 
 @pytest.fixture(scope="module", autouse=True)
@@ -44,3 +44,30 @@ def test_bits(rows, cols):
     same_bits(*quantise(x, gain))
     same_bits(*quantise(x, None))
 
+
+@pytest.mark.parametrize("rows,cols", SIZES)
+def test_gain_beyond_the_range(rows, cols):
+    """x gain leaves float32's range, above and below, where y does not."""
+    g = torch.Generator(device="cuda").manual_seed(cols)
+    x = 1 + torch.rand(rows, cols, generator=g, device="cuda")
+    # squares beyond float32: 1/rms is 0, and so is y
+    y, q, s = quantise(1e30 * x, torch.full((cols,), 1e10, device="cuda"))
+    assert not bool(y.any()) and not bool(q.float().any()) and bool((s == 2.0 ** -126).all())
+    y, q, s = quantise(1e15 * x, torch.full((cols,), 1e25, device="cuda"))
+    assert bool((y > 1e24).all()) and bool(torch.isfinite(y).all())
+    same_bits(y, q, s)
+    y, q, s = quantise(1e-18 * x, torch.full((cols,), 1e-25, device="cuda"), eps=0.0)
+    assert bool((y > 1e-26).all()) and bool((y < 1e-24).all())
+    same_bits(y, q, s)
+
+
+@pytest.mark.parametrize("rows,cols", SIZES)
+def test_infinite_scale(rows, cols):
+    """An infinity among finite y: the scale is infinite, the finite ones stand at 0."""
+    x, gain = torch.ones(rows, cols, device="cuda"), torch.ones(cols, device="cuda")
+    x[:, 7], gain[7] = 4.0, 3e38
+    y, q, s = quantise(x, gain)
+    assert bool(torch.isinf(y[:, 7]).all()) and bool(torch.isinf(s).all())
+    assert bool(torch.isnan(q[:, 7].float()).all())
+    rest = torch.arange(cols) != 7
+    assert bool(torch.isfinite(y[:, rest]).all()) and not bool(q[:, rest].float().any())
