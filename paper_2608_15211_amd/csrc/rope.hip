@@ -7,9 +7,12 @@
 //
 // Angles.  position * f_i loses every digit that counts in float32 at far
 // positions, so a frequency comes as turns a position in 64-bit fixed point
-// and the product is taken modulo 2^64, which drops the whole turns exactly:
-// an angle is off by at most |position| * 2^-65 turns besides the float32
-// steps after it, at any 32-bit position.
+// and the product is taken modulo 2^64, which drops the whole turns exactly.  A
+// frequency is within 1.5 * 2^-64 turns of its formula (YaRN 2.8 at the usual betas:
+// half a unit of its rounding, and the long double steps before it), so an angle is
+// off by at most 2.8 |position| 2^-64 turns, and by 2^-32 turns more where the
+// product is cut to its upper half: below 6e-10 turns at any 32-bit position,
+// besides the float32 steps after it.
 //
 // What bounds it: HBM, every channel is read and written once.  A workgroup
 // takes `tb` tokens: it first works out their cosines and sines, once for all
@@ -186,16 +189,16 @@ hipError_t rope_t(const RopeArgs& a, int v, bool half, hipStream_t st) {
 void rope_turns(double base, int scaling, double factor, double orig_len, double beta_fast, double beta_slow, int part,
                 uint64_t* turns) {
   const long double two_pi = 6.283185307179586476925286766559005768L;
-  if (scaling == 2) base *= pow(factor, (double)part / (part - 2));
+  const long double b = scaling == 2 ? base * powl(factor, (long double)part / (part - 2)) : base;
   for (int i = 0; i < part / 2; ++i) {
-    long double f = powl((long double)base, -2.0L * i / part) / two_pi;
+    long double f = powl(b, -2.0L * i / part) / two_pi;
     if (scaling == 1) f /= factor;
     if (scaling == 3) {
       long double keep = (orig_len * f - beta_slow) / (beta_fast - beta_slow);
       keep = keep < 0 ? 0 : keep > 1 ? 1 : keep;
       f *= keep + (1 - keep) / factor;
     }
-    turns[i] = (uint64_t)ldexpl(f, 64);
+    turns[i] = (uint64_t)rintl(ldexpl(f, 64));
   }
 }
 
