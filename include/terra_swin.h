@@ -407,7 +407,8 @@ typedef struct terra_rmsnorm_desc {
 int terra_rmsnorm_fwd(const terra_rmsnorm_desc* d, int dtype, const void* x, const void* res, const float* gain,
                       void* z, void* y, void* q, float* q_scale, float* rstd, void* stream);
 
-/* Device workspace terra_rmsnorm_bwd needs for dgain (0 on invalid input). */
+/* Device workspace terra_rmsnorm_bwd needs for dgain, for up to `rows` rows (0
+ * on invalid input). */
 size_t terra_rmsnorm_bwd_workspace_bytes(int64_t rows, int32_t cols);
 
 /* Backward from dy (gradient of y; stride y_ld) and dz (nullable: what reaches
@@ -432,7 +433,10 @@ typedef struct terra_linear_desc {
 } terra_linear_desc;
 
 /* Workspaces of the linear layer's calls, for these sizes and any strides and
- * addresses (0 on invalid input; the forward often needs none). */
+ * addresses (0 on invalid input; the forward often needs none).  They do not
+ * grow with M: few tokens may need more than many, since products of few tiles
+ * are summed in slices, so a workspace for several sizes takes the largest of
+ * their answers. */
 size_t terra_linear_fwd_workspace_bytes(int64_t M, int32_t N, int32_t K, int dtype);
 size_t terra_linear_bwd_workspace_bytes(int64_t M, int32_t N, int32_t K, int dtype);
 

@@ -660,7 +660,7 @@ int terra_rmsnorm_fwd(const terra_rmsnorm_desc* d, int dtype, const void* x, con
 
 size_t terra_rmsnorm_bwd_workspace_bytes(int64_t rows, int32_t cols) {
   if (rows < 0 || cols < 1) return 0;
-  return (size_t)terra::rms_bwd_blocks(rows, cols) * cols * sizeof(float);
+  return (size_t)terra::rms_bwd_most_blocks(rows, cols) * cols * sizeof(float);
 }
 
 int terra_rmsnorm_bwd(const terra_rmsnorm_desc* d, int dtype, const void* dy, const void* z, const float* rstd,
@@ -679,7 +679,7 @@ int terra_rmsnorm_bwd(const terra_rmsnorm_desc* d, int dtype, const void* dy, co
   }
   if ((s = check_mats({{"dgain", dgain, d->cols, d->cols, 4}}))) return s;
   if (dgain && d->rows > 0) {
-    const size_t need = terra_rmsnorm_bwd_workspace_bytes(d->rows, d->cols);
+    const size_t need = (size_t)terra::rms_bwd_blocks(d->rows, d->cols) * d->cols * sizeof(float);
     if (!workspace || workspace_bytes < need)
       return fail(TERRA_ERR_WORKSPACE, "workspace of %zu bytes needed, %zu given", need, workspace ? workspace_bytes : 0);
     if ((uintptr_t)workspace % 16) return fail(TERRA_ERR_INVALID, "workspace must be 16-byte aligned");

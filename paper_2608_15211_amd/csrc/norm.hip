@@ -13,6 +13,8 @@
 // What bounds it: HBM, a row is read once and stays in registers.  A row is
 // held by TPR threads (one wave, 256 or 1024 threads), thread t with the
 // 8-element chunks t, t + TPR, ... (NCH of them).
+#include <algorithm>
+
 #include "terra_vec.h"
 #include "terra_ops.h"
 
@@ -452,10 +454,11 @@ __global__ __launch_bounds__(1024) void part_sum_kernel(const float* __restrict_
 struct RowForm {
   int tpr, nch;           // tpr 0: the long form
 };
+constexpr int64_t kFewRows = 1024;
 RowForm row_form(int64_t rows, int cols, int most) {
   const int chunks = (cols + 7) / 8;
   auto pick = [&](int tpr) { return RowForm{tpr, chunks <= tpr ? 1 : 2}; };
-  if (chunks <= 64 || (chunks <= 128 && rows > 1024)) return pick(64);
+  if (chunks <= 64 || (chunks <= 128 && rows > kFewRows)) return pick(64);
   if (chunks <= 512) return pick(256);
   if (chunks <= 1024) return RowForm{512, 2};
   if (chunks <= 1024 * most) return RowForm{1024, 2};
@@ -519,8 +522,12 @@ hipError_t launch_part_sum(const float* part, float* out, int n, int cols, hipSt
   return hipGetLastError();
 }
 
-// Workgroups of the backward, each with a row of partial sums.
+// Workgroups of the backward, each with a row of partial sums; and the most for up to
+// so many rows (the form for few rows can have more than that for many).
 int rms_bwd_blocks(int64_t rows, int cols) { return row_blocks(rows, row_form(rows, cols, kBwdMost), true); }
+int rms_bwd_most_blocks(int64_t rows, int cols) {
+  return std::max(rms_bwd_blocks(rows, cols), rms_bwd_blocks(std::min<int64_t>(rows, kFewRows), cols));
+}
 
 hipError_t launch_rms_fwd(int dtype, const RmsFwd& a, hipStream_t st) {
   if (a.rows == 0) return hipSuccess;

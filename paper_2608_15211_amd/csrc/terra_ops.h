@@ -31,6 +31,7 @@ struct RmsBwd {
 hipError_t launch_part_sum(const float* part, float* out, int n, int cols, hipStream_t st);
 
 int rms_bwd_blocks(int64_t rows, int cols);
+int rms_bwd_most_blocks(int64_t rows, int cols);
 hipError_t launch_rms_fwd(int dtype, const RmsFwd& a, hipStream_t st);
 hipError_t launch_rms_bwd(int dtype, RmsBwd a, float* dgain, hipStream_t st);
 

@@ -220,6 +220,7 @@ def terra_rmsnorm_fwd(x, gain=None, res=None, eps=1e-5, out=None, z=None, rstd=N
 
 
 def terra_rmsnorm_bwd_workspace_bytes(rows, cols):
+    """Workspace of terra_rmsnorm_bwd for up to `rows` rows."""
     return int(lib().terra_rmsnorm_bwd_workspace_bytes(rows, cols))
 
 
@@ -244,10 +245,12 @@ def terra_rmsnorm_bwd(dy, z, rstd, gain=None, dz=None, out=None, workspace=None)
 
 # ------------------------------------------------------------- linear layer
 def terra_linear_fwd_workspace_bytes(M, N, K, dtype):
+    """Workspace of terra_linear_fwd for these sizes; fewer tokens may need more."""
     return int(lib().terra_linear_fwd_workspace_bytes(M, N, K, _code(dtype)))
 
 
 def terra_linear_bwd_workspace_bytes(M, N, K, dtype):
+    """Workspace of terra_linear_bwd for these sizes; fewer tokens may need more."""
     return int(lib().terra_linear_bwd_workspace_bytes(M, N, K, _code(dtype)))
 
 
