@@ -609,13 +609,14 @@ int terra_winattn_bwd_nhwc_noalloc(const terra_geom* g, int dtype, const void* q
 
 // ---- root-mean-square norm ------------------------------------------------
 
+constexpr int32_t kMaxCols = 1 << 24;
 static int check_rms(const terra_rmsnorm_desc* d, int dtype) {
   if (!d) return fail(TERRA_ERR_INVALID, "descriptor pointer is NULL");
   int s = check_dtype(dtype);
   if (s) return s;
   if (d->rows < 0 || d->cols < 1) return fail(TERRA_ERR_INVALID, "rows must be >= 0 and cols >= 1");
   if (!(d->eps >= 0.0f && d->eps < INFINITY)) return fail(TERRA_ERR_INVALID, "eps must be finite and >= 0");
-  if (d->cols > (1 << 24)) return fail(TERRA_ERR_UNSUPPORTED, "cols must be at most 2^24");
+  if (d->cols > kMaxCols) return fail(TERRA_ERR_UNSUPPORTED, "cols must be at most 2^24");
   return ok();
 }
 
@@ -659,7 +660,7 @@ int terra_rmsnorm_fwd(const terra_rmsnorm_desc* d, int dtype, const void* x, con
 }
 
 size_t terra_rmsnorm_bwd_workspace_bytes(int64_t rows, int32_t cols) {
-  if (rows < 0 || cols < 1) return 0;
+  if (rows < 0 || cols < 1 || cols > kMaxCols) return 0;
   return (size_t)terra::rms_bwd_most_blocks(rows, cols) * cols * sizeof(float);
 }
 
@@ -848,7 +849,8 @@ static int rope_common(const terra_rope_plan* p, int dtype, int64_t tokens, cons
   terra::RopeArgs a = {};
   const int es = dtype == TERRA_F32 ? 4 : 2;
   const terra_rope_tensor* t[2] = {q, k};
-  int heads = 0;
+  if ((int64_t)q->heads + (k ? k->heads : 0) > 256)
+    return fail(TERRA_ERR_UNSUPPORTED, "more than 256 heads of q and k together");
   for (int i = 0; i < 2; ++i) {
     if (!t[i]) continue;
     const char* name = i == 0 ? "q" : "k";
@@ -867,9 +869,7 @@ static int rope_common(const terra_rope_plan* p, int dtype, int64_t tokens, cons
     if (t[i]->in == t[i]->out && (in_h != out_h || in_t != out_t))
       return fail(TERRA_ERR_INVALID, "%s: in place, input and output must have the same strides", name);
     a.side[i] = {t[i]->in, t[i]->out, t[i]->heads, in_t, in_h, out_t, out_h};
-    heads += t[i]->heads;
   }
-  if (heads > 256) return fail(TERRA_ERR_UNSUPPORTED, "more than 256 heads of q and k together");
   a.tokens = tokens;
   a.pos = pos;
   a.axes = d.axes;

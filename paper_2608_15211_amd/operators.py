@@ -95,6 +95,12 @@ def _choice(value, choices, name):
         raise ValueError("%s must be one of %s, not %r" % (name, ", ".join(choices), value)) from None
 
 
+def _i32(n):
+    """A size for one of the library's 32-bit integers, which ctypes would cut to its low bits:
+    what does not fit becomes the largest, and that is refused."""
+    return n if -0x80000000 <= n < 0x80000000 else 0x7fffffff
+
+
 def _on(t, name, device, dtype):
     if t.get_device() != device:
         raise ValueError("%s is on %s, expected cuda:%d" % (name, t.device, device))
@@ -214,14 +220,14 @@ def terra_rmsnorm_fwd(x, gain=None, res=None, eps=1e-5, out=None, z=None, rstd=N
     (xp, xl), (rp, rl) = _matrix(x, "x", dev, dt, rows, C), _matrix(res, "res", dev, dt, rows, C)
     (zp, zl), (yp, yl) = _matrix(z, "z", dev, dt, rows, C), _matrix(out, "out", dev, dt, rows, C)
     qp, ql = _matrix(q, "q", dev, torch.float8_e4m3fn, rows, C)
-    _call(lib().terra_rmsnorm_fwd, dev, terra_rmsnorm_desc(rows, C, eps, xl, rl, zl, yl, ql), _code(dt), xp, rp,
+    _call(lib().terra_rmsnorm_fwd, dev, terra_rmsnorm_desc(rows, _i32(C), eps, xl, rl, zl, yl, ql), _code(dt), xp, rp,
           _vector(gain, "gain", dev, C), zp, yp, qp, _vector(q_scale, "q_scale", dev, rows), _vector(rstd, "rstd", dev, rows))
     return out, z
 
 
 def terra_rmsnorm_bwd_workspace_bytes(rows, cols):
     """Workspace of terra_rmsnorm_bwd for up to `rows` rows."""
-    return int(lib().terra_rmsnorm_bwd_workspace_bytes(rows, cols))
+    return int(lib().terra_rmsnorm_bwd_workspace_bytes(rows, _i32(cols)))
 
 
 def terra_rmsnorm_bwd(dy, z, rstd, gain=None, dz=None, out=None, workspace=None):
@@ -235,10 +241,10 @@ def terra_rmsnorm_bwd(dy, z, rstd, gain=None, dz=None, out=None, workspace=None)
         out = (torch.empty(dy.shape, dtype=dt, device=dy.device),
                None if gain is None else torch.empty(C, dtype=torch.float32, device=dy.device))
     dx, dgain = out
-    ws, wp, wn = _workspace(workspace, lambda: 0 if dgain is None else lib().terra_rmsnorm_bwd_workspace_bytes(rows, C), dev)
+    ws, wp, wn = _workspace(workspace, lambda: 0 if dgain is None else lib().terra_rmsnorm_bwd_workspace_bytes(rows, _i32(C)), dev)
     (yp, yl), (zp, zl) = _matrix(dy, "dy", dev, dt, rows, C), _matrix(z, "z", dev, dt, rows, C)
     (rp, rl), (xp, xl) = _matrix(dz, "dz", dev, dt, rows, C), _matrix(dx, "dx", dev, dt, rows, C)
-    _call(lib().terra_rmsnorm_bwd, dev, terra_rmsnorm_desc(rows, C, 0.0, xl, rl, zl, yl, 0), _code(dt), yp, zp,
+    _call(lib().terra_rmsnorm_bwd, dev, terra_rmsnorm_desc(rows, _i32(C), 0.0, xl, rl, zl, yl, 0), _code(dt), yp, zp,
           _vector(rstd, "rstd", dev, rows), _vector(gain, "gain", dev, C), rp, xp, _vector(dgain, "dgain", dev, C), wp, wn)
     return dx, dgain
 
@@ -246,12 +252,12 @@ def terra_rmsnorm_bwd(dy, z, rstd, gain=None, dz=None, out=None, workspace=None)
 # ------------------------------------------------------------- linear layer
 def terra_linear_fwd_workspace_bytes(M, N, K, dtype):
     """Workspace of terra_linear_fwd for these sizes; fewer tokens may need more."""
-    return int(lib().terra_linear_fwd_workspace_bytes(M, N, K, _code(dtype)))
+    return int(lib().terra_linear_fwd_workspace_bytes(M, _i32(N), _i32(K), _code(dtype)))
 
 
 def terra_linear_bwd_workspace_bytes(M, N, K, dtype):
     """Workspace of terra_linear_bwd for these sizes; fewer tokens may need more."""
-    return int(lib().terra_linear_bwd_workspace_bytes(M, N, K, _code(dtype)))
+    return int(lib().terra_linear_bwd_workspace_bytes(M, _i32(N), _i32(K), _code(dtype)))
 
 
 def terra_linear_fwd(x, w, bias=None, act="none", res=None, x_scale=None, w_scale=None, out=None, pre=None,
@@ -273,8 +279,8 @@ def terra_linear_fwd(x, w, bias=None, act="none", res=None, x_scale=None, w_scal
     (xp, xl), (wp, wl) = _matrix(x, "x", dev, dt, M, K), _matrix(w, "w", dev, dt, N, K)
     (yp, yl), (rp, rl) = _matrix(out, "out", dev, to, M, N), _matrix(res, "res", dev, to, M, N)
     pp, pl = _matrix(pre, "pre", dev, to, M, N)
-    ws, sp, sn = _workspace(workspace, lambda: lib().terra_linear_fwd_workspace_bytes(M, N, K, code), dev)
-    _call(lib().terra_linear_fwd, dev, terra_linear_desc(M, N, K, xl, wl, yl, rl, pl, 0, 0, _choice(act, _ACTS, "act"), _code(to)),
+    ws, sp, sn = _workspace(workspace, lambda: lib().terra_linear_fwd_workspace_bytes(M, _i32(N), _i32(K), code), dev)
+    _call(lib().terra_linear_fwd, dev, terra_linear_desc(M, _i32(N), _i32(K), xl, wl, yl, rl, pl, 0, 0, _choice(act, _ACTS, "act"), _code(to)),
           code, xp, _vector(x_scale, "x_scale", dev, M), wp, _vector(w_scale, "w_scale", dev, N),
           _vector(bias, "bias", dev, N), rp, yp, pp, sp, sn)
     return out
@@ -297,8 +303,8 @@ def terra_linear_bwd(dy, x, w, pre=None, act="none", out=None, workspace=None):
     (yp, yl), (xp, xl) = _matrix(dy, "dy", dev, dt, M, N), _matrix(x, "x", dev, dt, M, K)
     (wp, wl), (pp, pl) = _matrix(w, "w", dev, dt, N, K), _matrix(pre, "pre", dev, dt, M, N)
     (ip, il), (gp, gl) = _matrix(dx, "dx", dev, dt, M, K), _matrix(dw, "dw", dev, dt if dw is None or dw.dtype == dt else torch.float32, N, K)
-    ws, sp, sn = _workspace(workspace, lambda: lib().terra_linear_bwd_workspace_bytes(M, N, K, code), dev)
-    _call(lib().terra_linear_bwd, dev, terra_linear_desc(M, N, K, xl, wl, yl, 0, pl, il, gl, _choice(act, _ACTS, "act"), code), code,
+    ws, sp, sn = _workspace(workspace, lambda: lib().terra_linear_bwd_workspace_bytes(M, _i32(N), _i32(K), code), dev)
+    _call(lib().terra_linear_bwd, dev, terra_linear_desc(M, _i32(N), _i32(K), xl, wl, yl, 0, pl, il, gl, _choice(act, _ACTS, "act"), code), code,
           yp, xp, wp, pp, ip, gp, TERRA_F32 if dw is None else _code(dw.dtype), _vector(db, "dbias", dev, N), sp, sn)
     return out
 
@@ -310,7 +316,7 @@ def terra_plan_rope(head_dim, rot_dim=None, axes=1, layout="half", base=10000.0,
     first rot_dim (default: all) channels of a head turn, in `axes` (1 or 2)
     equal parts, pairs interleaved or in halves; frequencies base^(-2i/part),
     scaled for long contexts (none, linear, ntk, yarn) by `factor`."""
-    d = terra_rope_desc(head_dim, head_dim if rot_dim is None else rot_dim, axes, _choice(layout, _LAYOUTS, "layout"),
+    d = terra_rope_desc(_i32(head_dim), _i32(head_dim if rot_dim is None else rot_dim), _i32(axes), _choice(layout, _LAYOUTS, "layout"),
                         _choice(scaling, _SCALINGS, "scaling"), base, factor, orig_len, beta_fast, beta_slow, attn_scale)
     plan = terra_rope_plan()
     _check(lib().terra_plan_rope(d, plan))
@@ -333,7 +339,7 @@ def _heads(x, out, name, tokens, hd, device, dtype):
             if t.stride(-1) != 1:
                 raise ValueError("%s must be contiguous along its last dimension" % (name if t is x else name + "'s output"))
             steps += (_step(t.shape[:-2], t.stride()[:-2], name) or 0, t.stride(-2))
-    return terra_rope_tensor(x.data_ptr(), out.data_ptr(), heads, *steps)
+    return terra_rope_tensor(x.data_ptr(), out.data_ptr(), _i32(heads), *steps)
 
 
 def _rope(fn, plan, q, k, pos, grid, out):
@@ -351,7 +357,7 @@ def _rope(fn, plan, q, k, pos, grid, out):
             raise ValueError("pos must be contiguous with %d x %d elements" % (tokens, plan.desc.axes))
     elif grid is None:
         raise ValueError("pos or grid must be given")
-    h, w = (0, 0) if grid is None else grid
+    h, w = (0, 0) if grid is None else (_i32(grid[0]), _i32(grid[1]))
     _call(fn, dev, plan, _code(dt), tokens, None if pos is None else pos.data_ptr(), h, w, tq, tk)
     return out
 
