@@ -402,8 +402,9 @@ typedef struct terra_rmsnorm_desc {
  *   q_scale = max(max |y| / 448, 2^-126),  q = y / q_scale (the float32
  *   quotient) to nearest even,
  * so that q * q_scale stands for y.  A NaN in a row makes its scale and the
- * row's y NaN.  z may be x or res, and y may be x, in place with the same
- * stride (not both the same). */
+ * row's y NaN.  z and y may each be x or res, in place with the same stride
+ * (not both the same one: TERRA_ERR_INVALID).  Squares beyond float32's range
+ * make rstd 0. */
 int terra_rmsnorm_fwd(const terra_rmsnorm_desc* d, int dtype, const void* x, const void* res, const float* gain,
                       void* z, void* y, void* q, float* q_scale, float* rstd, void* stream);
 
@@ -416,8 +417,9 @@ size_t terra_rmsnorm_bwd_workspace_bytes(int64_t rows, int32_t cols);
  * them: with g = dy gain and zh = z rstd,
  *   dx = rstd (g - zh mean(g zh)) + dz   (`dtype`; of x and of res alike; x_ld)
  *   dgain = sum over rows of dy zh       (float32, cols; overwritten)
- * dx or dgain may be NULL; workspace is needed with dgain.  dx may be dy or
- * dz in place.  The sum over rows has a fixed order (bit-reproducible). */
+ * dx or dgain may be NULL; workspace is needed with dgain.  dx may be dy, z or
+ * dz in place with the same stride.  The sum over rows has a fixed order
+ * (bit-reproducible). */
 int terra_rmsnorm_bwd(const terra_rmsnorm_desc* d, int dtype, const void* dy, const void* z, const float* rstd,
                       const float* gain, const void* dz, void* dx, float* dgain, void* workspace,
                       size_t workspace_bytes, void* stream);
@@ -446,7 +448,8 @@ size_t terra_linear_bwd_workspace_bytes(int64_t M, int32_t N, int32_t K, int dty
  * x w^T x_scale[m] w_scale[n] (out_dtype TERRA_BF16 or TERRA_F16).  Sums are
  * float32.  bias float32 (N), res M x N, both nullable; pre (nullable, M x N)
  * receives t for the backward.  GELU is the exact (erf) form, SiLU
- * t / (1 + exp(-t)).  y may be res in place with the same stride. */
+ * t / (1 + exp(-t)).  y or pre may be res in place with the same stride; no
+ * output may be x or w, or both the same (TERRA_ERR_INVALID). */
 int terra_linear_fwd(const terra_linear_desc* d, int dtype, const void* x, const float* x_scale, const void* w,
                      const float* w_scale, const float* bias, const void* res, void* y, void* pre, void* workspace,
                      size_t workspace_bytes, void* stream);
@@ -458,7 +461,8 @@ int terra_linear_fwd(const terra_linear_desc* d, int dtype, const void* x, const
  * each nullable, one at least, overwritten.  `dtype` is TERRA_BF16 or
  * TERRA_F16.  pre is needed unless act is TERRA_ACT_NONE.  dt enters the two
  * products rounded to `dtype` (exact for TERRA_ACT_NONE), and dbias in
- * float32.  Sums over tokens have a fixed order (bit-reproducible). */
+ * float32.  Sums over tokens have a fixed order (bit-reproducible).  No output
+ * may be an input that the call reads (TERRA_ERR_INVALID). */
 int terra_linear_bwd(const terra_linear_desc* d, int dtype, const void* dy, const void* x, const void* w,
                      const void* pre, void* dx, void* dw, int dw_dtype, float* dbias, void* workspace,
                      size_t workspace_bytes, void* stream);
@@ -508,8 +512,8 @@ typedef struct terra_rope_tensor {
  * NULL: token t of the grid_h x grid_w grid (t taken modulo its tokens) is at
  * row t / grid_w, column t % grid_w, on one axis at t.  Element types
  * TERRA_F32, TERRA_BF16, TERRA_F16, angles to float32's precision at any
- * position.  `out` may be `in` with the same strides.  At most 256 heads of q
- * and k together. */
+ * position.  `out` may be `in` with the same strides, but not the other tensor's.
+ * At most 256 heads of q and k together. */
 int terra_rope_fwd(const terra_rope_plan* plan, int dtype, int64_t tokens, const int32_t* pos, int32_t grid_h,
                    int32_t grid_w, const terra_rope_tensor* q, const terra_rope_tensor* k, void* stream);
 

@@ -641,6 +641,20 @@ static int check_mats(std::initializer_list<MatArg> mats) {
   return ok();
 }
 
+// Outputs at an input's address.  `out` may not be any of `others`:
+static int check_apart(const char* name, const void* out, std::initializer_list<MatArg> others) {
+  for (const MatArg& m : others)
+    if (out && out == m.p) return fail(TERRA_ERR_INVALID, "%s and %s are the same memory", name, m.name);
+  return ok();
+}
+// `out` may be one of `inputs` if its rows are the same ones.
+static int check_in_place(const MatArg& out, int64_t rows, std::initializer_list<MatArg> inputs) {
+  for (const MatArg& m : inputs)
+    if (out.p && out.p == m.p && out.ld != m.ld && rows > 1)
+      return fail(TERRA_ERR_INVALID, "%s is %s in place with another row stride", out.name, m.name);
+  return ok();
+}
+
 int terra_rmsnorm_fwd(const terra_rmsnorm_desc* d, int dtype, const void* x, const void* res, const float* gain,
                       void* z, void* y, void* q, float* q_scale, float* rstd, void* stream) {
   int s = check_rms(d, dtype);
@@ -650,9 +664,13 @@ int terra_rmsnorm_fwd(const terra_rmsnorm_desc* d, int dtype, const void* x, con
   if (!q != !q_scale) return fail(TERRA_ERR_INVALID, "q and q_scale come together");
   if (!z && !y && !q && !rstd) return fail(TERRA_ERR_INVALID, "no output asked for");
   const int es = dtype == TERRA_F32 ? 4 : 2;
-  if ((s = check_mats({{"x", x, d->x_ld, d->cols, es}, {"res", res, d->res_ld, d->cols, es},
-                       {"z", z, d->z_ld, d->cols, es}, {"y", y, d->y_ld, d->cols, es}, {"q", q, d->q_ld, d->cols, 1},
-                       {"gain", gain, d->cols, d->cols, 4}, {"q_scale", q_scale, 1, 1, 4}, {"rstd", rstd, 1, 1, 4}})))
+  const MatArg mx = {"x", x, d->x_ld, d->cols, es}, mr = {"res", res, d->res_ld, d->cols, es},
+               mz = {"z", z, d->z_ld, d->cols, es}, my = {"y", y, d->y_ld, d->cols, es};
+  if ((s = check_mats({mx, mr, mz, my, {"q", q, d->q_ld, d->cols, 1}, {"gain", gain, d->cols, d->cols, 4},
+                       {"q_scale", q_scale, 1, 1, 4}, {"rstd", rstd, 1, 1, 4}})))
+    return s;
+  if ((s = check_apart("y", y, {mz})) || (s = check_apart("q", q, {mx, mr, mz, my})) ||
+      (s = check_in_place(mz, d->rows, {mx, mr})) || (s = check_in_place(my, d->rows, {mx, mr})))
     return s;
   terra::RmsFwd a = {x, res, gain, z, y, (uint8_t*)q, q_scale, rstd, d->rows, d->x_ld, d->res_ld, d->z_ld, d->y_ld,
                      d->q_ld, d->cols, d->eps};
@@ -673,9 +691,10 @@ int terra_rmsnorm_bwd(const terra_rmsnorm_desc* d, int dtype, const void* dy, co
   const int es = dtype == TERRA_F32 ? 4 : 2;
   if (d->rows > 0) {
     if (!dy || !z || !rstd) return fail(TERRA_ERR_INVALID, "dy, z or rstd is NULL");
-    if ((s = check_mats({{"dy", dy, d->y_ld, d->cols, es}, {"z", z, d->z_ld, d->cols, es},
-                         {"dz", dz, d->res_ld, d->cols, es}, {"dx", dx, d->x_ld, d->cols, es},
-                         {"gain", gain, d->cols, d->cols, 4}, {"rstd", rstd, 1, 1, 4}})))
+    const MatArg my = {"dy", dy, d->y_ld, d->cols, es}, mz = {"z", z, d->z_ld, d->cols, es},
+                 mr = {"dz", dz, d->res_ld, d->cols, es}, mx = {"dx", dx, d->x_ld, d->cols, es};
+    if ((s = check_mats({my, mz, mr, mx, {"gain", gain, d->cols, d->cols, 4}, {"rstd", rstd, 1, 1, 4}})) ||
+        (s = check_in_place(mx, d->rows, {my, mz, mr})))
       return s;
   }
   if ((s = check_mats({{"dgain", dgain, d->cols, d->cols, 4}}))) return s;
@@ -742,11 +761,15 @@ int terra_linear_fwd(const terra_linear_desc* d, int dtype, const void* x, const
   if (q ? (!x_scale || !w_scale) : (x_scale || w_scale))
     return fail(TERRA_ERR_INVALID, "x_scale and w_scale come with TERRA_E4M3 operands, and only with them");
   const int es = q ? 1 : 2;
-  if ((s = check_mats({{"x", x, d->x_ld, d->K, es}, {"w", w, d->w_ld, d->K, es}, {"y", y, d->y_ld, d->N, 2},
-                       {"res", res, d->res_ld, d->N, 2}, {"pre", pre, d->pre_ld, d->N, 2},
-                       {"bias", bias, d->N, d->N, 4}, {"x_scale", x_scale, 1, 1, 4}, {"w_scale", w_scale, 1, 1, 4}})))
+  const MatArg mx = {"x", x, d->x_ld, d->K, es}, mw = {"w", w, d->w_ld, d->K, es}, my = {"y", y, d->y_ld, d->N, 2},
+               mr = {"res", res, d->res_ld, d->N, 2}, mp = {"pre", pre, d->pre_ld, d->N, 2};
+  if ((s = check_mats({mx, mw, my, mr, mp, {"bias", bias, d->N, d->N, 4}, {"x_scale", x_scale, 1, 1, 4},
+                       {"w_scale", w_scale, 1, 1, 4}})))
     return s;
   if ((s = check_linear_ws(terra::lin_fwd_workspace(d->M, d->N, d->K, dtype), workspace, workspace_bytes))) return s;
+  if ((s = check_apart("y", y, {mx, mw, mp})) || (s = check_apart("pre", pre, {mx, mw})) ||
+      (s = check_in_place(my, d->M, {mr})) || (s = check_in_place(mp, d->M, {mr})))
+    return s;
   terra::LinFwd a = {x, w, x_scale, w_scale, bias, res, y, pre, d->M, d->x_ld, d->w_ld, d->y_ld, d->res_ld, d->pre_ld,
                      d->N, d->K, d->act};
   return hip_status(terra::launch_lin_fwd(dtype, d->out_dtype, a, workspace, (hipStream_t)stream),
@@ -770,18 +793,21 @@ int terra_linear_bwd(const terra_linear_desc* d, int dtype, const void* dy, cons
   if (!dx && !dw && !dbias) return fail(TERRA_ERR_INVALID, "no output asked for");
   if (dw && dw_dtype != TERRA_F32 && dw_dtype != dtype)
     return fail(TERRA_ERR_INVALID, "dw_dtype %d is neither TERRA_F32 nor the element type", dw_dtype);
+  // the inputs that are read
+  const MatArg my = {"dy", dy, d->y_ld, d->N, 2}, mx = {"x", dw ? x : nullptr, d->x_ld, d->K, 2},
+               mw = {"w", dx ? w : nullptr, d->w_ld, d->K, 2},
+               mp = {"pre", d->act != TERRA_ACT_NONE ? pre : nullptr, d->pre_ld, d->N, 2};
   if (d->M > 0) {
     if (!dy || (dw && !x) || (dx && !w)) return fail(TERRA_ERR_INVALID, "dy, x or w is NULL");
     if (d->act != TERRA_ACT_NONE && !pre) return fail(TERRA_ERR_INVALID, "pre is NULL, and act is not TERRA_ACT_NONE");
-    if ((s = check_mats({{"dy", dy, d->y_ld, d->N, 2}, {"x", dw ? x : nullptr, d->x_ld, d->K, 2},
-                         {"w", dx ? w : nullptr, d->w_ld, d->K, 2},
-                         {"pre", d->act != TERRA_ACT_NONE ? pre : nullptr, d->pre_ld, d->N, 2},
-                         {"dx", dx, d->dx_ld, d->K, 2}})))
-      return s;
+    if ((s = check_mats({my, mx, mw, mp, {"dx", dx, d->dx_ld, d->K, 2}}))) return s;
   }
   if ((s = check_mats({{"dw", dw, d->dw_ld, d->K, dw_dtype == TERRA_F32 ? 4 : 2}, {"dbias", dbias, d->N, d->N, 4}})))
     return s;
   if ((s = check_linear_ws(terra::lin_bwd_workspace(d->M, d->N, d->K), workspace, workspace_bytes))) return s;
+  if (d->M > 0 && ((s = check_apart("dx", dx, {my, mx, mw, mp})) ||
+                   (s = check_apart("dw", dw, {my, mx, mw, mp, {"dx", dx, d->dx_ld, d->K, 2}}))))
+    return s;
   terra::LinBwd a = {dy, x, w, pre, dx, dw, dbias, d->M, d->y_ld, d->x_ld, d->w_ld, d->pre_ld, d->dx_ld, d->dw_ld,
                      d->N, d->K, d->act, dw_dtype == TERRA_F32};
   return hip_status(terra::launch_lin_bwd(dtype, a, workspace, (hipStream_t)stream), "terra_linear_bwd launch");
@@ -870,6 +896,8 @@ static int rope_common(const terra_rope_plan* p, int dtype, int64_t tokens, cons
       return fail(TERRA_ERR_INVALID, "%s: in place, input and output must have the same strides", name);
     a.side[i] = {t[i]->in, t[i]->out, t[i]->heads, in_t, in_h, out_t, out_h};
   }
+  if (k && tokens > 0 && (q->out == k->out || q->out == k->in || k->out == q->in))
+    return fail(TERRA_ERR_INVALID, "an output of q or k is the same memory as the other's input or output");
   a.tokens = tokens;
   a.pos = pos;
   a.axes = d.axes;
