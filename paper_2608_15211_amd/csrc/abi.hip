@@ -317,6 +317,9 @@ int terra_internal_wgrad_plan(int T, int Nl, int Kl) { return terra::block_wgrad
 int terra_internal_linear_form(int64_t M, int N, int K, int dtype, int aligned) {
   return terra::lin_form(M, N, K, dtype, aligned != 0);
 }
+int terra_internal_linear_few_waves(int64_t M, int N, int K, int dtype) {
+  return terra::lin_few_waves(M, N, K, dtype);
+}
 int terra_internal_linear_wgrad_form(int64_t M, int N, int K, int aligned) {
   return terra::lin_wgrad_form(M, N, K, aligned != 0);
 }

@@ -66,6 +66,26 @@ __device__ __forceinline__ void stage_products(f32x16 (&acc)[MI][2], const bf16x
   }
 }
 
+// Up to 16 bytes of a row, `left` of them inside it, the rest zero.
+template <int ES>
+__device__ inline i32x4 row_tail(const char* p, int left) {
+  i32x4 v = {0, 0, 0, 0};
+  if (left >= 16) {
+    __builtin_memcpy(&v, p, 16);
+    return v;
+  }
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    uint32_t x = 0;
+#pragma unroll
+    for (int i = 0; i < 4; i += ES)
+      if (4 * w + i < left)
+        x |= (ES == 2 ? (uint32_t)*reinterpret_cast<const uint16_t*>(p + 4 * w + i)
+                      : (uint32_t)*reinterpret_cast<const uint8_t*>(p + 4 * w + i)) << (8 * i);
+    v[w] = (int)x;
+  }
+  return v;
+}
 
 // ---------------------------------------------------------------------------
 // Operands of any alignment and length: 16-byte chunks pass through registers
@@ -87,22 +107,7 @@ struct RegStager {
       const bool row_in = KROW ? mr < outer : mr < kend;
       const int left = KROW ? min(row_bytes, 2 * kend) - 2 * mc : 2 * (outer - mc);
       v[u] = i32x4{0, 0, 0, 0};
-      if (!row_in || left <= 0) continue;
-      const char* src = p + (int64_t)mr * ld + 2 * mc;
-      if (left >= 16) {
-        __builtin_memcpy(&v[u], src, 16);
-      } else {
-#pragma unroll
-        for (int w = 0; w < 4; ++w) {
-          uint32_t x = 0;
-#pragma unroll
-          for (int i = 0; i < 4; i += ES)
-            if (4 * w + i < left)
-              x |= (ES == 2 ? (uint32_t)*reinterpret_cast<const uint16_t*>(src + 4 * w + i)
-                            : (uint32_t)*reinterpret_cast<const uint8_t*>(src + 4 * w + i)) << (8 * i);
-          v[u][w] = (int)x;
-        }
-      }
+      if (row_in && left > 0) v[u] = row_tail<ES>(p + (int64_t)mr * ld + 2 * mc, left);
     }
   }
   __device__ void store(bf16* tile) const {
@@ -608,8 +613,6 @@ __global__ __launch_bounds__(256) void slices_kernel(const float* __restrict__ p
 // lane l holds row l % 16, bytes 16 (l / 16) and 64 further on), and their sums
 // are added through LDS in wave order.  No barrier stands between the loads.
 // ---------------------------------------------------------------------------
-typedef _Float16 half8 __attribute__((ext_vector_type(8)));
-
 template <typename T>
 __device__ inline void skinny_mma(f32x4& acc, const i32x4 (&a)[2], const i32x4 (&b)[2]) {
   if constexpr (std::is_same<T, e4m3>::value) {
@@ -625,27 +628,6 @@ __device__ inline void skinny_mma(f32x4& acc, const i32x4 (&a)[2], const i32x4 (
         acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a[j]), __builtin_bit_cast(f16x8, b[j]), acc, 0, 0, 0);
     }
   }
-}
-
-// Up to 16 bytes of a row, `left` of them inside it, the rest zero.
-template <int ES>
-__device__ inline i32x4 row_tail(const char* p, int left) {
-  i32x4 v = {0, 0, 0, 0};
-  if (left >= 16) {
-    __builtin_memcpy(&v, p, 16);
-    return v;
-  }
-#pragma unroll
-  for (int w = 0; w < 4; ++w) {
-    uint32_t x = 0;
-#pragma unroll
-    for (int i = 0; i < 4; i += ES)
-      if (4 * w + i < left)
-        x |= (ES == 2 ? (uint32_t)*reinterpret_cast<const uint16_t*>(p + 4 * w + i)
-                      : (uint32_t)*reinterpret_cast<const uint8_t*>(p + 4 * w + i)) << (8 * i);
-    v[w] = (int)x;
-  }
-  return v;
 }
 
 struct SkinnyArgs {
@@ -1015,45 +997,62 @@ void skip_rows(GemmArgs& g, int64_t rows) {
   if (e.x_scale != nullptr) e.x_scale += rows;
 }
 
-// A product along memory rows: few tiles by plan_product; many as the rows of
-// whole rounds of one 256 x 256 tile a compute unit, and the rest by itself.
+// A product along memory rows: few tiles by plan_product; many as the first rows, in whole
+// rounds of one 256 x 256 tile a compute unit, and the rest (in one slice: `part` may
+// not hold more) by itself.
+struct RowPlan {
+  Plan p, rest;
+  int64_t first;         // 0: all of it by p
+};
+RowPlan plan_rows(int64_t M, int N, int K, bool direct) {
+  RowPlan r = {plan_product(M, N, K, kMaxSplit, direct), {}, 0};
+  if (r.p.nw == 8) r.first = first_rows(M, N, K, &r.rest);
+  return r;
+}
 template <typename T, typename TO>
 hipError_t row_product(GemmArgs g, float* part, hipStream_t st) {
   const bool direct = direct_ok(g.a, g.lda, kBM) && direct_ok(g.b, g.ldb, kBM) && g.row_bytes % 16 == 0;
-  Plan p = plan_product(g.M, g.N, g.K, kMaxSplit, direct);
-  if (p.nw == 8) {
-    Plan rest;
-    const int64_t rows = first_rows(g.M, g.N, g.K, &rest);
-    if (rows > 0) {
-      GemmArgs first = g;
-      first.M = rows;
-      const hipError_t e = product_form<T, TO, true>(first, Plan{8, 1}, false, nullptr, st);
-      if (e != hipSuccess) return e;
-      skip_rows<TO>(g, first.M);
-      p = rest;                                             // in one slice: `part` may not hold more
-    }
-  }
-  return product_form<T, TO, true>(g, p, false, part, st);
+  const RowPlan r = plan_rows(g.M, g.N, g.K, direct);
+  if (r.first == 0) return product_form<T, TO, true>(g, r.p, false, part, st);
+  GemmArgs first = g;
+  first.M = r.first;
+  const hipError_t e = product_form<T, TO, true>(first, r.p, false, part, st);
+  if (e != hipSuccess) return e;
+  skip_rows<TO>(g, r.first);
+  return product_form<T, TO, true>(g, r.rest, false, part, st);
 }
 
-template <typename T, typename TO, int MT>
-hipError_t skinny_rt(const SkinnyArgs& g, hipStream_t st) {
-  const int its = (g.row_bytes + 127) / 128;
-  const int rt = (g.N + 15) / 16 >= 4 * kCus ? 2 : 1;
-  // four pieces a wave, whose loads go out together, while there are 16 waves
-  int waves = 16;
-  while (waves > 4 && waves * 4 > its) waves /= 2;
-  while (waves > 1 && waves > its) waves /= 2;
-  const dim3 grid((g.N + 16 * rt - 1) / (16 * rt));
-  const size_t lds = (size_t)waves * MT * rt * 16 * kRedS * sizeof(float);
-  if (rt == 2) hipLaunchKernelGGL((skinny_kernel<T, TO, MT, 2>), grid, dim3(64 * waves), lds, st, g);
-  else hipLaunchKernelGGL((skinny_kernel<T, TO, MT, 1>), grid, dim3(64 * waves), lds, st, g);
+// Few tokens: tiles of tokens and of outputs a workgroup, and its waves: four pieces of a
+// row each, whose loads go out together, while there are 16 waves.
+struct FewPlan {
+  int mt, rt, waves;
+};
+FewPlan plan_few(int64_t M, int N, int row_bytes) {
+  const int its = (row_bytes + 127) / 128;
+  FewPlan p = {M <= 16 ? 1 : M <= 32 ? 2 : 4, (N + 15) / 16 >= 4 * kCus ? 2 : 1, 16};
+  while (p.waves > 4 && p.waves * 4 > its) p.waves /= 2;
+  while (p.waves > 1 && p.waves > its) p.waves /= 2;
+  return p;
+}
+
+template <typename T, typename TO, int MT, int RT>
+hipError_t skinny_launch(const SkinnyArgs& g, int waves, hipStream_t st) {
+  const size_t lds = (size_t)waves * MT * RT * 16 * kRedS * sizeof(float);
+  hipLaunchKernelGGL((skinny_kernel<T, TO, MT, RT>), dim3((g.N + 16 * RT - 1) / (16 * RT)), dim3(64 * waves), lds, st, g);
   return hipGetLastError();
 }
 
 template <typename T, typename TO>
 hipError_t skinny(const SkinnyArgs& g, hipStream_t st) {
-  return g.M <= 16 ? skinny_rt<T, TO, 1>(g, st) : g.M <= 32 ? skinny_rt<T, TO, 2>(g, st) : skinny_rt<T, TO, 4>(g, st);
+  const FewPlan p = plan_few(g.M, g.N, g.row_bytes);
+  switch (10 * p.mt + p.rt) {
+    case 11: return skinny_launch<T, TO, 1, 1>(g, p.waves, st);
+    case 12: return skinny_launch<T, TO, 1, 2>(g, p.waves, st);
+    case 21: return skinny_launch<T, TO, 2, 1>(g, p.waves, st);
+    case 22: return skinny_launch<T, TO, 2, 2>(g, p.waves, st);
+    case 41: return skinny_launch<T, TO, 4, 1>(g, p.waves, st);
+    default: return skinny_launch<T, TO, 4, 2>(g, p.waves, st);
+  }
 }
 
 size_t split_floats(int64_t M, int N, int K, bool direct) {
@@ -1206,14 +1205,17 @@ hipError_t bwd_t(const LinBwd& a, char* ws, hipStream_t st) {
 // for two of outputs; else 100 nw + slices, + 1000 where the rows are padded first,
 // + 10000 for whole rounds and a rest.
 int lin_form(int64_t M, int N, int K, int dtype, bool aligned) {
-  if (M <= kSkinnyMost) return (M <= 16 ? 1 : M <= 32 ? 2 : 4) + ((N + 15) / 16 >= 4 * kCus ? 10 : 0);
   const int row_bytes = dtype == kE4m3 ? K : 2 * K;
-  const bool padded = fwd_ws(M, N, row_bytes).padded, direct = padded || (aligned && row_bytes % 16 == 0);
-  const int ku = padded ? (row_bytes + 15) / 16 * 8 : (row_bytes + 1) / 2;
-  const Plan p = plan_product(M, N, ku, kMaxSplit, direct);
-  Plan rest;
-  return 100 * p.nw + p.ns + (padded ? 1000 : 0) + (p.nw == 8 && first_rows(M, N, ku, &rest) > 0 ? 10000 : 0);
+  if (M <= kSkinnyMost) {
+    const FewPlan p = plan_few(M, N, row_bytes);
+    return p.mt + (p.rt == 2 ? 10 : 0);
+  }
+  const bool padded = fwd_ws(M, N, row_bytes).padded;
+  const RowPlan r = plan_rows(M, N, padded ? (row_bytes + 15) / 16 * 8 : (row_bytes + 1) / 2, padded || (aligned && row_bytes % 16 == 0));
+  return 100 * r.p.nw + r.p.ns + (padded ? 1000 : 0) + (r.first > 0 ? 10000 : 0);
 }
+// Of a call with few tokens: its waves a workgroup.
+int lin_few_waves(int64_t M, int N, int K, int dtype) { return plan_few(M, N, dtype == kE4m3 ? K : 2 * K).waves; }
 // Of a weight gradient: 100 nw + slices.
 int lin_wgrad_form(int64_t M, int N, int K, bool aligned) {
   const Plan p = plan_wgrad(M, N, K, aligned);

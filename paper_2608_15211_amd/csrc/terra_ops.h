@@ -87,6 +87,7 @@ struct LinBwd {
 };
 
 int lin_form(int64_t M, int N, int K, int dtype, bool aligned);
+int lin_few_waves(int64_t M, int N, int K, int dtype);
 int lin_wgrad_form(int64_t M, int N, int K, bool aligned);
 size_t lin_fwd_workspace(int64_t M, int N, int K, int dtype);
 size_t lin_bwd_workspace(int64_t M, int N, int K);
