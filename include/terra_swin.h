@@ -446,10 +446,12 @@ size_t terra_linear_bwd_workspace_bytes(int64_t M, int32_t N, int32_t K, int dty
  * TERRA_BF16 or TERRA_F16 (out_dtype the same), or TERRA_E4M3 with x_scale
  * (float32, M) and w_scale (float32, N), whose products are
  * x w^T x_scale[m] w_scale[n] (out_dtype TERRA_BF16 or TERRA_F16).  Sums are
- * float32.  bias float32 (N), res M x N, both nullable; pre (nullable, M x N)
- * receives t for the backward.  GELU is the exact (erf) form, SiLU
- * t / (1 + exp(-t)).  y or pre may be res in place with the same stride; no
- * output may be x or w, or both the same (TERRA_ERR_INVALID). */
+ * float32; of TERRA_E4M3 operands each eight products along K first lose what is
+ * 13 bits below the leading one of the largest (8.5e-4 of it at most).  bias
+ * float32 (N), res M x N, both nullable; pre (nullable, M x N) receives t for
+ * the backward.  GELU is the exact (erf) form, SiLU t / (1 + exp(-t)).  y or
+ * pre may be res in place with the same stride; no output may be x or w, or
+ * both the same (TERRA_ERR_INVALID). */
 int terra_linear_fwd(const terra_linear_desc* d, int dtype, const void* x, const float* x_scale, const void* w,
                      const float* w_scale, const float* bias, const void* res, void* y, void* pre, void* workspace,
                      size_t workspace_bytes, void* stream);
@@ -482,7 +484,9 @@ enum terra_rope_scaling { TERRA_ROPE_PLAIN = 0, TERRA_ROPE_LINEAR = 1, TERRA_ROP
  *   YARN    f_i (g + (1 - g) / s), g = clamp((r - beta_slow) / (beta_fast -
  *           beta_slow), 0, 1), r = orig_len f_i / (2 pi) turns over the
  *           original length; cosine and sine times 0.1 ln(s) + 1
- * attn_scale > 0 replaces the factor on cosine and sine. */
+ * attn_scale > 0 replaces the factor on cosine and sine.  YARN's g is linear in
+ * the turns r; models trained with a ramp linear in the pair's index have other
+ * angles. */
 typedef struct terra_rope_desc {
   int32_t head_dim, rot_dim, axes, layout, scaling;
   double base, factor, orig_len, beta_fast, beta_slow, attn_scale;

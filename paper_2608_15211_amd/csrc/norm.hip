@@ -11,8 +11,8 @@
 // dx is the gradient of x and of res alike.
 //
 // What bounds it: HBM, a row is read once and stays in registers.  A row is
-// held by TPR threads (one wave, 256 or 1024 threads), thread t with the
-// 8-element chunks t, t + TPR, ... (NCH of them).
+// held by TPR threads (one wave, 256, 512 or, forward, 1024 threads), thread t with the
+// 8-element chunks t, t + TPR, ... (NCH of them); longer rows are read again.
 #include <algorithm>
 
 #include "terra_vec.h"
@@ -446,25 +446,24 @@ __global__ __launch_bounds__(1024) void part_sum_kernel(const float* __restrict_
 }
 
 // Threads a row and chunks a thread (one or two: with four the backward's
-// sums, the row and its successor no longer fit the registers).  One wave a row up
-// to 1024 columns, where rows are many: a row's sums then need no barrier.  Few
-// rows, and longer ones, take a workgroup each (9479 rows of 6751 into e4m3: 512
-// threads 131 us, 1024 threads 167).  `most`: chunks a thread at 1024
-// threads, which have 128 registers each.
+// sums, the row and its successor no longer fit the registers, nor with two at
+// 1024 threads, which have 128 registers each).  One wave a row up to 1024 columns,
+// where rows are many: a row's sums then need no barrier.  Few rows, and longer
+// ones, take a workgroup each (9479 rows of 6751 into e4m3: 512 threads 131 us,
+// 1024 threads 167).
 struct RowForm {
   int tpr, nch;           // tpr 0: the long form
 };
 constexpr int64_t kFewRows = 1024;
-RowForm row_form(int64_t rows, int cols, int most) {
+RowForm row_form(int64_t rows, int cols, bool fwd) {
   const int chunks = (cols + 7) / 8;
   auto pick = [&](int tpr) { return RowForm{tpr, chunks <= tpr ? 1 : 2}; };
   if (chunks <= 64 || (chunks <= 128 && rows > kFewRows)) return pick(64);
   if (chunks <= 512) return pick(256);
   if (chunks <= 1024) return RowForm{512, 2};
-  if (chunks <= 1024 * most) return RowForm{1024, 2};
+  if (chunks <= 2048 && fwd) return RowForm{1024, 2};
   return RowForm{0, 0};
 }
-constexpr int kFwdMost = 2, kBwdMost = 1;
 
 }  // namespace
 
@@ -494,7 +493,7 @@ int row_blocks(int64_t rows, const RowForm& f, bool bwd) {
 
 template <typename T>
 hipError_t fwd_t(const RmsFwd& a, hipStream_t st) {
-  const RowForm f = row_form(a.rows, a.cols, kFwdMost);
+  const RowForm f = row_form(a.rows, a.cols, true);
   const dim3 grid(row_blocks(a.rows, f, false));
   if (f.tpr == 0) hipLaunchKernelGGL(rms_fwd_long_kernel<T>, grid, dim3(1024), 0, st, a);
   TERRA_ROW_FORMS(rms_fwd_kernel, T)
@@ -505,7 +504,7 @@ hipError_t fwd_t(const RmsFwd& a, hipStream_t st) {
 
 template <typename T>
 hipError_t bwd_t(const RmsBwd& a, int blocks, hipStream_t st) {
-  const RowForm f = row_form(a.rows, a.cols, kBwdMost);
+  const RowForm f = row_form(a.rows, a.cols, false);
   const dim3 grid(blocks);
   if (f.tpr == 0) hipLaunchKernelGGL(rms_bwd_long_kernel<T>, grid, dim3(1024), 0, st, a);
   TERRA_ROW_FORMS(rms_bwd_kernel, T)
@@ -524,7 +523,7 @@ hipError_t launch_part_sum(const float* part, float* out, int n, int cols, hipSt
 
 // Workgroups of the backward, each with a row of partial sums; and the most for up to
 // so many rows (the form for few rows can have more than that for many).
-int rms_bwd_blocks(int64_t rows, int cols) { return row_blocks(rows, row_form(rows, cols, kBwdMost), true); }
+int rms_bwd_blocks(int64_t rows, int cols) { return row_blocks(rows, row_form(rows, cols, false), true); }
 int rms_bwd_most_blocks(int64_t rows, int cols) {
   return std::max(rms_bwd_blocks(rows, cols), rms_bwd_blocks(std::min<int64_t>(rows, kFewRows), cols));
 }

@@ -1,5 +1,5 @@
 // terra_ops.h - argument blocks of the operators around the attention
-// (norm.hip, linear.hip, rope.hip), filled by the C ABI (abi_ops.hip).
+// (norm.hip, linear.hip, rope.hip), filled by the C ABI (abi.hip).
 #pragma once
 
 #include <hip/hip_runtime.h>
