@@ -771,7 +771,7 @@ hipError_t pad_rows(const PadArgs& a, hipStream_t st) {
 // the runs of rows.  32 threads along 256 columns, eight rows at a time.
 // The rounding is what lets dx and dW be 16-bit products at the matrix cores' rate (in
 // two 16-bit parts they would take twice the time).  With an activation it makes
-// their error against 64 bits 2.3e-3 (norm over norm, bf16 outputs; 1.7e-3 by the
+// their error against 64 bits 2.4e-3 (norm over norm, bf16 outputs; 1.7e-3 by the
 // outputs' own rounding alone); without one dt is dy and nothing is lost.
 template <typename T>
 struct ActGrad {
